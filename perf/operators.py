@@ -22,7 +22,7 @@ own = False
 _DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
 _BLOCK = 128
 _E4M3_MAX = 448.0
-_LEAST_AMAX = 2.0 ** -100   # a block of smaller values is scaled as if this were its largest
+_LEAST_AMAX = 2.0 ** -60   # a block of smaller values is scaled as if this were its largest
 
 
 def _case(name, kind, experts, n, k, rows, dtype="bf16", zipf=0.0, **more):
