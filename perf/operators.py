@@ -236,7 +236,7 @@ def work(case):
 def _nearest_e4m3(v):
     """float64 -> the nearest value of e4m3 (ties to even), as float64.  Steps of 2^-3 of the leading power of two, 2^-9 below 2^-6."""
     _, exponent = torch.frexp(v)
-    step = torch.ldexp(torch.ones_like(v), (exponent - 1).clamp_min(-6) - 3)
+    step = ((exponent.long() - 1).clamp_min(-6) - 3 + 1023).bitwise_left_shift(52).view(torch.float64)   # (pow(2, n) may be off)
     return torch.round(v / step) * step
 
 
