@@ -1,0 +1,75 @@
+// Shared by the translation units of the grouped products (include/moe_products.h): arguments, launchers and how a workgroup
+// finds its tile.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "moe_internal.h"
+#include "moe_products.h"
+
+namespace moe {
+namespace products {
+
+// What a product computes, as out[row, feature] = sum over c of q(row, c) * p(feature, c):
+//   kForward  q = x,  p = W_e,    c = in_features
+//   kDgrad    q = dy, p = W_e^T,  c = out_features
+//   kWgrad    q = dy^T, p = x^T,  c = the rows of expert e; an output matrix for every expert
+enum Form { kForward, kDgrad, kWgrad };
+
+struct Args {
+    const void *q, *p;
+    void* out;
+    const int32_t* offsets;           // [E + 1], or null: one expert with all rows
+    int experts, rows, n, k;          // n = out_features, k = in_features
+    const float *q_scales, *p_scales; // 8-bit operands, else null
+    int accumulate;                   // kWgrad
+};
+
+// First and one past the last row of lane `lane`'s expert, inside [0, rows] whatever the table holds.
+__device__ inline void expert_rows(const Args& a, int lane, int& first, int& end) {
+    first = end = 0;
+    if (lane < a.experts) {
+        first = a.offsets == nullptr ? 0 : min(max(a.offsets[lane], 0), a.rows);
+        end = a.offsets == nullptr ? a.rows : min(max(a.offsets[lane + 1], first), a.rows);
+    }
+}
+
+// Row tiles of at most `height` rows that a call can have, which the host knows without the table: every expert's last one may be ragged.
+inline long most_row_tiles(int rows, int experts, int height) {
+    return (rows + height - 1) / height + (experts - 1 < rows ? experts - 1 : rows);
+}
+
+// Row tile `tile` of `height` rows (the same in all lanes; expert by expert): its expert, first row and rows; false if there is none.
+__device__ inline bool find_row_tile(const Args& a, int tile, int height, int& expert, int& row0, int& rows) {
+    const int lane = threadIdx.x & 63;
+    int first, end;
+    expert_rows(a, lane, first, end);
+    const int tiles = (end - first + height - 1) / height;
+    int sum = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int u = __shfl_up(sum, d, 64);
+        if (lane >= d) sum += u;
+    }
+    if (tile >= __builtin_amdgcn_readlane(sum, 63)) return false;
+    expert = __popcll(__ballot(sum <= tile));
+    const int m = tile - __builtin_amdgcn_readlane(sum - tiles, expert);
+    const int end_row = __builtin_amdgcn_readlane(end, expert);
+    row0 = __builtin_amdgcn_readlane(first, expert) + m * height;
+    rows = min(height, end_row - row0);
+    return true;
+}
+
+// Each enqueues a whole product and returns hipGetLastError().  `workspace`: product_workspace_bytes() of scratch.
+hipError_t launch_f32(Form form, const Args& a, hipStream_t stream);
+hipError_t launch_bf16(Form form, const Args& a, bool out_f32, void* workspace, hipStream_t stream);
+hipError_t launch_fp8(const Args& a, void* workspace, hipStream_t stream);
+size_t product_workspace_bytes(const moe_product_t& p, int rows);
+
+hipError_t launch_quantize_rows(int rows, int features, int dtype, const void* x, uint8_t* q, float* scales, hipStream_t stream);
+hipError_t launch_quantize_weights(const moe_product_t& p, const void* w, uint8_t* q, float* scales, uint8_t* q_t, float* scales_t,
+                                   hipStream_t stream);
+
+}  // namespace products
+}  // namespace moe
