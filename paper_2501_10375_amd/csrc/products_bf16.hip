@@ -1,0 +1,35 @@
+// Launches of the grouped bf16 products, see products_bf16.h.
+#include "products_bf16.h"
+
+namespace moe {
+namespace products {
+namespace {
+
+constexpr size_t kScratchBytes = kScratchUnits * kUnitFloats * sizeof(float);
+
+template <int FORM, bool OUT32>
+hipError_t launch(const Args& a, void* workspace, hipStream_t stream) {
+    float* scratch = static_cast<float*>(workspace);
+    Plan* plan = reinterpret_cast<Plan*>(static_cast<char*>(workspace) + kScratchBytes);
+    const int grid = max(kXcds, compute_units() / kXcds * kXcds);
+    product_gemm_kernel<FORM, OUT32><<<grid, 256, 0, stream>>>(a, scratch, plan);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    join_pieces_kernel<FORM, OUT32><<<kScratchUnits / 8 * 8, 256, 0, stream>>>(a, scratch, plan);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_bf16(Form form, const Args& a, bool out_f32, void* workspace, hipStream_t stream) {
+    switch (form) {
+        case kForward: return launch<kForward, false>(a, workspace, stream);
+        case kDgrad: return launch<kDgrad, false>(a, workspace, stream);
+        default: return out_f32 ? launch<kWgrad, true>(a, workspace, stream) : launch<kWgrad, false>(a, workspace, stream);
+    }
+}
+
+size_t product_workspace_bytes(const moe_product_t& p, int) { return p.dtype == MOE_F32 ? 256 : kScratchBytes + 256; }
+
+}  // namespace products
+}  // namespace moe

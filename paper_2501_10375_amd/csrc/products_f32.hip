@@ -191,14 +191,7 @@ hipError_t launch_form(Form form, const Args& a, hipStream_t stream) {
 
 hipError_t launch_f32(Form form, const Args& a, hipStream_t stream) { return launch_form<float, float>(form, a, stream); }
 
-hipError_t launch_bf16(Form form, const Args& a, bool out_f32, void*, hipStream_t stream) {
-    if (out_f32) return launch<uint16_t, float, kWgrad, 64>(a, stream);
-    return launch_form<uint16_t, uint16_t>(form, a, stream);
-}
-
 hipError_t launch_fp8(const Args& a, void*, hipStream_t stream) { return launch<uint8_t, uint16_t, kForward, 64>(a, stream); }
-
-size_t product_workspace_bytes(const moe_product_t&, int) { return 256; }
 
 }  // namespace products
 }  // namespace moe
