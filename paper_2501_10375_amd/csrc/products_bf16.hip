@@ -5,17 +5,15 @@ namespace moe {
 namespace products {
 namespace {
 
-constexpr size_t kScratchBytes = kScratchUnits * kUnitFloats * sizeof(float);
-
 template <int FORM, bool OUT32>
 hipError_t launch(const Args& a, void* workspace, hipStream_t stream) {
     float* scratch = static_cast<float*>(workspace);
     Plan* plan = reinterpret_cast<Plan*>(static_cast<char*>(workspace) + kScratchBytes);
-    const int grid = max(kXcds, compute_units() / kXcds * kXcds);
+    const int grid = persistent_grid();
     product_gemm_kernel<FORM, OUT32><<<grid, 256, 0, stream>>>(a, scratch, plan);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    join_pieces_kernel<FORM, OUT32><<<kScratchUnits / 8 * 8, 256, 0, stream>>>(a, scratch, plan);
+    join_pieces_kernel<FORM, kStepC, OUT32><<<kMostCutTiles * 8, 256, 0, stream>>>(a, scratch, plan);
     return hipGetLastError();
 }
 

@@ -191,7 +191,5 @@ hipError_t launch_form(Form form, const Args& a, hipStream_t stream) {
 
 hipError_t launch_f32(Form form, const Args& a, hipStream_t stream) { return launch_form<float, float>(form, a, stream); }
 
-hipError_t launch_fp8(const Args& a, void*, hipStream_t stream) { return launch<uint8_t, uint16_t, kForward, 64>(a, stream); }
-
 }  // namespace products
 }  // namespace moe

@@ -61,6 +61,12 @@ __device__ inline bool find_row_tile(const Args& a, int tile, int height, int& e
     return true;
 }
 
+// Workgroups of a persistent launch: one a CU, a multiple of the 8 XCDs.
+inline int persistent_grid() {
+    const int n = compute_units() / 8 * 8;
+    return n < 8 ? 8 : n > 256 ? 256 : n;
+}
+
 // Each enqueues a whole product and returns hipGetLastError().  `workspace`: product_workspace_bytes() of scratch.
 hipError_t launch_f32(Form form, const Args& a, hipStream_t stream);
 hipError_t launch_bf16(Form form, const Args& a, bool out_f32, void* workspace, hipStream_t stream);
