@@ -52,7 +52,7 @@ int enqueue(products::Form form, const moe_product_t& p, int32_t rows, const voi
             void* out, bool out_f32, int accumulate, void* workspace, void* hip_stream) {
     const Args a = {q, second, out, offsets, p.n_experts, rows, p.out_features, p.in_features, nullptr, nullptr, accumulate};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (form == products::kForward && p.dtype == MOE_BF16 && rows <= products::kFewRows) return status(products::launch_few_rows(a, false, stream));
+    if (form == products::kForward && p.dtype == MOE_BF16 && products::few_rows(a, false)) return status(products::launch_few_rows(a, false, stream));
     return status(p.dtype == MOE_F32 ? products::launch_f32(form, a, stream) : products::launch_bf16(form, a, out_f32, workspace, stream));
 }
 
@@ -127,7 +127,7 @@ int moe_grouped_product_fp8(const moe_product_t* product, int32_t rows, const ui
     if (rows == 0) return MOE_OK;
     const Args a = {xq, wq, y, offsets, product->n_experts, rows, product->out_features, product->in_features, x_scales, w_scales, 0};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    return status(rows <= products::kFewRows ? products::launch_few_rows(a, true, stream) : products::launch_fp8(a, workspace, stream));
+    return status(products::few_rows(a, true) ? products::launch_few_rows(a, true, stream) : products::launch_fp8(a, workspace, stream));
 }
 
 }  // extern "C"

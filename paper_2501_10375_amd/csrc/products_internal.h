@@ -71,8 +71,8 @@ inline int persistent_grid() {
 hipError_t launch_f32(Form form, const Args& a, hipStream_t stream);
 hipError_t launch_bf16(Form form, const Args& a, bool out_f32, void* workspace, hipStream_t stream);
 hipError_t launch_fp8(const Args& a, void* workspace, hipStream_t stream);
-// Forward products of at most kFewRows rows, of bf16 or (with scales) e4m3 matrices.
-constexpr int kFewRows = 32;
+// Forward products of few rows, of bf16 or (with scales) e4m3 matrices, and which calls have few.
+bool few_rows(const Args& a, bool fp8);
 hipError_t launch_few_rows(const Args& a, bool fp8, hipStream_t stream);
 size_t product_workspace_bytes(const moe_product_t& p, int rows);
 
