@@ -23,7 +23,7 @@
  *   - offsets == NULL, with n_experts == 1: all rows belong to the one expert (a
  *     plain product).
  *   - Limits: out_features and in_features are multiples of 64 up to 1048576,
- *     n_experts <= 64, rows <= 8388608, and one expert's matrix has at most 2^31
+ *     n_experts <= 64, rows <= 8388608, and one expert's matrix has less than 2^31
  *     elements.
  *   - rows == 0 is MOE_OK; the per-row buffers may then be NULL.
  *   - Sums are held in fp32 (one rounding to the output's type).  For fp32

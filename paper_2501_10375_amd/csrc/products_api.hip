@@ -15,7 +15,7 @@ int check_product(const moe_product_t* p) {
     if (p == nullptr) return MOE_ERR_NULL;
     if (p->dtype != MOE_F32 && p->dtype != MOE_BF16) return MOE_ERR_DTYPE;
     if (bad_features(p->out_features) || bad_features(p->in_features)) return MOE_ERR_SHAPE;
-    if ((int64_t)p->out_features * p->in_features > (int64_t)1 << 31) return MOE_ERR_SHAPE;
+    if ((int64_t)p->out_features * p->in_features >= (int64_t)1 << 31) return MOE_ERR_SHAPE;
     if (p->n_experts < 1 || p->n_experts > 64) return MOE_ERR_SHAPE;
     return MOE_OK;
 }

@@ -37,9 +37,37 @@ struct TileKernel {
     using Yes = std::true_type;
     using No = std::false_type;
 
-    static __device__ GG_INLINE void set_lds_target(uint32_t a) { asm volatile("s_mov_b32 m0, %0" ::"s"(a) : "memory"); }
-    static __device__ GG_INLINE void load_lane(u32x4 d, uint32_t off) {
-        asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(d) : "memory");
+    // M0 (the LDS address of the load that follows behind some other instruction) ...
+    static __device__ GG_INLINE void set_lds_target(uint32_t to) { asm volatile("s_mov_b32 m0, %0" ::"s"(to) : "memory"); }
+    // ... and the load itself: 16 bytes a lane from the buffer to M0 + lane * 16.
+    static __device__ GG_INLINE void load_lane(u32x4 d, uint32_t off) { asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(d) : "memory"); }
+    static __device__ GG_INLINE void load_to(uint32_t to, u32x4 d, uint32_t off) {
+        set_lds_target(to);
+        asm volatile("s_nop 0" ::: "memory");
+        load_lane(d, off);
+    }
+    static constexpr uint32_t kNowhere = 0xc0000000u;  // a lane offset behind the end of every buffer
+    // Cache policy of results (the nt bit): they are not kept in favour of operands.  wgrad of 8 x 14336 x 4096: 512 rows an expert in fp32 691 ->
+    // 630 us, 64 rows in bf16 244 -> 198.
+    static constexpr int kStreamed = 2;
+    // Waits for the first two K steps of an item, which were requested before the `stores` of the item before.
+    // (The counter has six bits: with 64 behind them, what it can wait for is enough.)
+    static __device__ GG_INLINE void wait_first(int stores) {
+        switch (stores) {
+            case 0: gg::wait_vmcnt<0>(); break;
+            case 4: gg::wait_vmcnt<4>(); break;
+            case 8: gg::wait_vmcnt<8>(); break;
+            case 12: gg::wait_vmcnt<12>(); break;
+            case 16: gg::wait_vmcnt<16>(); break;
+            case 20: gg::wait_vmcnt<20>(); break;
+            case 24: gg::wait_vmcnt<24>(); break;
+            case 28: gg::wait_vmcnt<28>(); break;
+            case 32: gg::wait_vmcnt<32>(); break;
+            case 40: gg::wait_vmcnt<40>(); break;
+            case 48: gg::wait_vmcnt<48>(); break;
+            case 56: gg::wait_vmcnt<56>(); break;
+            default: gg::wait_vmcnt<63>(); break;
+        }
     }
     // See Gemm::mfma_acc() of the expert GEMMs for why the MFMAs are asm statements, and settle() and pin() around them.
     static __device__ GG_INLINE void mfma_acc(f32x4& acc, bf16x8 a, bf16x8 b) {
@@ -58,7 +86,6 @@ struct TileKernel {
         asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(a));
         return v;
     }
-    static __device__ GG_INLINE void wait_state() { asm volatile("s_nop 0" ::: "memory"); }
 
     // Half a fragment (4 c of 16 rows) out of a column stage.
     static __device__ GG_INLINE i16x4 read_turned(lds_ptr p) {
@@ -75,14 +102,12 @@ struct TileKernel {
         const int wave = uniform((int)threadIdx.x >> 6);
         const int wt = wave & 1, wq = wave >> 1;      // row group, feature group
         const uint32_t wave_lds = lds0 + (uint32_t)wave * 1024;
-        auto next_w = [](uint32_t s) GG_LAMBDA { return s == 2 * kStage ? 0u : s + kStage; };
 
         // ---- staging.  Rows: load n of wavefront w covers rows n * 32 + w * 8 .. + 7, lane l the 16-byte piece that belongs at
         // position l % 8 of row l / 8.  Columns: c n * 8 + w * 2 and the next one, lane l the piece that belongs at position l % 32 of
         // line l / 32; there 32-byte units are exchanged, unit u of line c at u ^ (c % 4 + 4 (c / 8 % 2)), so that the 32 lanes that a
         // transposing read serves at a time (eight c, 32 bytes each) find their units in different banks.
         const uint32_t p_ld = (uint32_t)K * 2u, q_ld = (uint32_t)(FORM == kForward ? K : N) * 2u;
-        const uint32_t p_step = kPCols ? kStepC * p_ld : kStepC * 2u, q_step = kQCols ? kStepC * q_ld : kStepC * 2u;
         uint32_t p_off[8], q_off[8];
         {
             const int lane = threadIdx.x & 63;
@@ -96,57 +121,51 @@ struct TileKernel {
             }
         }
         Buffer p, q;
-        auto p_load = [&](int n) GG_LAMBDA { load_lane(p.d, p_off[n]); };
-        auto q_load = [&](int n) GG_LAMBDA { load_lane(q.d, q_off[n]); };
-        auto q_loads = [](int rows) GG_LAMBDA { return kQCols ? 8 : (rows + 31) / 32; };
+        auto p_next = [&]() GG_LAMBDA {
+            if constexpr (kPCols) p.template next_columns<kStepC>();
+            else p.next_rows(kStepC * 2);
+        };
+        auto q_next = [&]() GG_LAMBDA {
+            if constexpr (kQCols) q.template next_columns<kStepC>();
+            else q.next_rows(kStepC * 2);
+        };
         auto p_stage = [&](uint32_t stage) GG_LAMBDA {
 #pragma unroll
-            for (int n = 0; n < 8; ++n) {
-                set_lds_target(wave_lds + stage + n * 4096);
-                wait_state();
-                p_load(n);
-            }
-            p.advance(p_step);
+            for (int n = 0; n < 8; ++n) load_to(wave_lds + stage + n * 4096, p.d, p_off[n]);
+            p_next();
         };
-        auto q_stage = [&](uint32_t stage, int loads) GG_LAMBDA {
+        auto q_stage = [&](uint32_t stage, int rows) GG_LAMBDA {
 #pragma unroll
-            for (int n = 0; n < 8; ++n) {
-                if (n >= loads) break;
-                set_lds_target(wave_lds + kQBase + stage + n * 4096);
-                wait_state();
-                q_load(n);
-            }
-            q.advance(q_step);
+            for (int n = 0; n < 8; ++n)
+                if (kQCols || n * 32 < rows) load_to(wave_lds + kQBase + stage + n * 4096, q.d, q_off[n]);
+            q_next();
         };
-        // First requests of an item, into p stage w0 and q stage 0.
-        auto request_first = [&](const Item& t, uint32_t w0) GG_LAMBDA {
+        // The first two K steps of an item.
+        auto request_first = [&](const Item& t) GG_LAMBDA {
             const uint16_t *pm = static_cast<const uint16_t*>(a.p), *qm = static_cast<const uint16_t*>(a.q);
             if constexpr (FORM == kWgrad) {
-                p.set(pm + (size_t)t.c0 * K + t.f0, ((int64_t)t.depth * K - t.f0) * 2);
-                q.set(qm + (size_t)t.c0 * N + t.row0, ((int64_t)t.depth * N - t.row0) * 2);
+                p.template set_columns<kStepC>(pm + (size_t)t.c0 * K + t.f0, t.depth, p_ld, (uint32_t)t.f0 * 2u, t.k_steps);
+                q.template set_columns<kStepC>(qm + (size_t)t.c0 * N + t.row0, t.depth, q_ld, (uint32_t)t.row0 * 2u, t.k_steps);
             } else {
-                const int64_t at = FORM == kForward ? (int64_t)t.f0 * K + t.c0 : (int64_t)t.c0 * K + t.f0;   // in the expert's matrix
-                p.set(pm + (size_t)t.expert * N * K + at, ((int64_t)N * K - at) * 2);
+                const uint16_t* matrix = pm + (size_t)t.expert * N * K;
+                if constexpr (kPCols) p.template set_columns<kStepC>(matrix + (size_t)t.c0 * K + t.f0, t.depth, p_ld, (uint32_t)t.f0 * 2u, t.k_steps);
+                else p.set_rows(matrix + (size_t)t.f0 * K + t.c0, ((int64_t)min(kTile, N - t.f0) * K - t.c0) * 2, t.k_steps);
                 const int ld = FORM == kForward ? K : N;
-                q.set(qm + (size_t)t.row0 * ld + t.c0, ((int64_t)t.rows * ld - t.c0) * 2);
+                q.set_rows(qm + (size_t)t.row0 * ld + t.c0, ((int64_t)t.rows * ld - t.c0) * 2, t.k_steps);
             }
-            p_stage(w0);
-            q_stage(0, q_loads(t.rows));
+            p_stage(0);
+            q_stage(0, t.rows);
+            p_stage(kStage);
+            q_stage(kStage, t.rows);
         };
 
-        uint32_t w0 = 0;   // p stage of an item's first K step
-        request_first(cur, w0);
+        int stores = 0;   // of the item before
+        request_first(cur);
         for (int n = 1;; ++n) {
         int tid = threadIdx.x;   // (opaque: lane addresses are computed where they are used)
         asm volatile("" : "+v"(tid));
         const int lane = tid & 63;
-        const int KT = cur.k_steps;
-        if (KT > 1) {
-            p_stage(next_w(w0));
-            gg::wait_vmcnt<8>();
-        } else {
-            gg::wait_vmcnt<0>();
-        }
+        wait_first(stores);
         gg::lds_barrier();
 
         // ---- fragments.  Rows: 16 rows x 32 c, lane l holds row l % 16, piece l / 16 of the half K step, at r * 128 + ((piece ^ ((r >> 1) & 7))
@@ -183,47 +202,37 @@ struct TileKernel {
             pin(acc);
             settle();
 
-            constexpr int kM = kF * TFE, kR = kF + TFE, kQLoads = kQCols ? 8 : TFE;
+            constexpr int kM = kF * TFE, kR = kF + TFE, kQLoads = kQCols ? 8 : TFE, kLoads = kQLoads + 8;
             bf16x8 pf[2][kF], qf[2][TFE];
-            // Half a K step: the MFMAs of fragment buffer mbuf, between them the LDS reads of half `half` of the stages
-            // into buffer 1 - mbuf, and the loads of one operand (LOADS 1: q, 2: p) for a later K step.
-            auto half_step = [&](auto mfma, auto mbuf_c, auto read, int half, uint32_t p_at, uint32_t q_at, auto loads, uint32_t target) GG_LAMBDA {
-                constexpr int mbuf = decltype(mbuf_c)::value, rbuf = 1 - mbuf;
-                constexpr int LOADS = decltype(loads)::value;
-                constexpr int n_loads = LOADS == 1 ? kQLoads : LOADS == 2 ? 8 : 1;
-                constexpr int gap = kM / n_loads;
+            // Half a K step: the MFMAs of fragment buffer mbuf, between them the LDS reads of half `half` of the stages p_at and q_at
+            // into buffer 1 - mbuf, and the loads of one operand (LOADS 1: q, 2: p) for a later K step into the stage `to`.
+            auto half_step = [&](auto mfma, auto mbuf_c, auto reads, int half, uint32_t p_at, uint32_t q_at, auto loads, uint32_t to) GG_LAMBDA {
+                constexpr int mbuf = decltype(mbuf_c)::value, rbuf = 1 - mbuf, LOADS = decltype(loads)::value;
+                constexpr int n_loads = LOADS == 1 ? kQLoads : 8;
                 constexpr int read_slots = kM - kM / 8;   // the last reads get some MFMAs' time before they are used
 #pragma unroll
                 for (int m = 0; m < kM; ++m) {
-                    if constexpr (decltype(mfma)::value) {
-                        const int i = m / kF, j = m % kF;
-                        mfma_acc(acc[j][i], pf[mbuf][j], qf[mbuf][i]);
-                    }
-                    if constexpr (decltype(read)::value) {
-#pragma unroll
-                        for (int x = 0; x < kR; ++x) {
-                            if (x * read_slots / kR != m) continue;
-                            if (x < kF) pf[rbuf][x] = fragment(std::bool_constant<kPCols>{}, p_read, p_at, half, x);
-                            else qf[rbuf][x - kF] = fragment(std::bool_constant<kQCols>{}, q_read, q_at + kQBase, half, (x - kF) * 2);
-                        }
-                    }
-                    if constexpr (LOADS != 0) {
-                        const int l = m / gap;
-                        if (l < n_loads) {
-                            if (m % gap == 0) {
-                                set_lds_target(target + l * 4096);
-                                if (gap == 1) wait_state();
-                            }
-                            if (m % gap == gap / 2) {
-                                if constexpr (LOADS == 1) q_load(l);
-                                else p_load(l);
-                            }
+                    // x of n things over `of` slots goes into slot x * of / n: a load at most, up to two reads
+                    const int l = (m * n_loads + kM - 1) / kM, r = (m * kR + read_slots - 1) / read_slots;
+                    const bool load = LOADS != 0 && l < n_loads && l * kM / n_loads == m;
+                    if (load) set_lds_target(wave_lds + (LOADS == 1 ? kQBase : 0) + to + l * 4096);
+                    if constexpr (decltype(mfma)::value) mfma_acc(acc[m % kF][m / kF], pf[mbuf][m % kF], qf[mbuf][m / kF]);
+                    auto read = [&](int x) GG_LAMBDA {
+                        if (!decltype(reads)::value || x >= kR || x * read_slots / kR != m) return;
+                        if (x < kF) pf[rbuf][x] = fragment(std::bool_constant<kPCols>{}, p_read, p_at, half, x);
+                        else qf[rbuf][x - kF] = fragment(std::bool_constant<kQCols>{}, q_read, q_at + kQBase, half, (x - kF) * 2);
+                    };
+                    read(r);
+                    read(r + 1);
+                    if (load) {
+                        load_lane(LOADS == 1 ? q.d : p.d, LOADS == 1 ? q_off[l] : p_off[l]);
+                        if (l == n_loads - 1) {
+                            if constexpr (LOADS == 1) q_next();
+                            else p_next();
                         }
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                if constexpr (LOADS == 1) q.advance(q_step);
-                if constexpr (LOADS == 2) p.advance(p_step);
             };
             using Buf0 = std::integral_constant<int, 0>;
             using Buf1 = std::integral_constant<int, 1>;
@@ -231,42 +240,45 @@ struct TileKernel {
             using LoadQ = std::integral_constant<int, 1>;
             using LoadP = std::integral_constant<int, 2>;
 
-            // first half of K step 0 into buffer 0; q of K step 1 requested
-            uint32_t p_at = w0, q_at = 0;                      // stages of K step kt
+            // First and second halves of the K steps in turn; while one is computed the next is read.  p of a step is requested in the first half of the one
+            // two before it, q in the second half.
+            uint32_t p_at = 0, q_at = 0, p_to = 2 * kStage;           // stages of K step kt, and where p of kt + 2 goes
             half_step(No{}, Buf1{}, Yes{}, 0, p_at, q_at, None{}, 0u);
-            if (KT > 1) q_stage(kStage, kQLoads);
-            auto k_step = [&](auto more) GG_LAMBDA {  // second half of K step kt, first half of K step kt + 1
-                const uint32_t w1 = next_w(p_at), w2 = next_w(w1), q1 = q_at ^ kStage;
-                // Stage w2 held K step kt - 1, which every wavefront had read before the last barrier.
-                half_step(Yes{}, Buf0{}, Yes{}, 1, p_at, q_at, std::conditional_t<decltype(more)::value, LoadP, None>{}, wave_lds + w2);
-                // Outstanding, oldest first: p of K step kt + 1, its q, p of K step kt + 2.
-                if constexpr (decltype(more)::value) gg::wait_vmcnt<8>();
-                else gg::wait_vmcnt<0>();
+            half_step(Yes{}, Buf0{}, Yes{}, 1, p_at, q_at, LoadP{}, p_to);
+            gg::lds_barrier();   // (step 1 is there: the stores of the item before are not waited for yet)
+            for (int kt = 0; kt < cur.k_steps - 1; ++kt) {
+                const uint32_t p1 = p_at == 2 * kStage ? 0u : p_at + kStage, q1 = q_at ^ kStage;
+                p_to = p_at;     // nobody reads step kt's stages any more
+                half_step(Yes{}, Buf1{}, Yes{}, 0, p1, q1, LoadQ{}, q_at);
+                half_step(Yes{}, Buf0{}, Yes{}, 1, p1, q1, LoadP{}, p_to);
+                // Outstanding, oldest first: p of kt + 2, q of kt + 2, p of kt + 3 (eight loads).
+                gg::wait_vmcnt<8>();
                 gg::lds_barrier();
-                half_step(Yes{}, Buf1{}, Yes{}, 0, w1, q1, std::conditional_t<decltype(more)::value, LoadQ, None>{}, wave_lds + kQBase + q_at);
-                p_at = w1;
+                p_at = p1;
                 q_at = q1;
-            };
-            for (int kt = 0; kt < KT - 2; ++kt) k_step(Yes{});
-            if (KT > 1) k_step(No{});
-            half_step(Yes{}, Buf0{}, Yes{}, 1, p_at, q_at, None{}, 0u);
+            }
             half_step(Yes{}, Buf1{}, No{}, 0, 0u, 0u, None{}, 0u);
             settle();
             pin(acc);
 
             // ---- the next item's first operands are requested before this one's results are stored.
             more_items = decode(n, next);
+            gg::wait_vmcnt<0>();
             gg::lds_barrier();   // every wavefront is done reading operand tiles; no load is outstanding
-            w0 = next_w(p_at);
-            if (more_items) request_first(next, w0);
+            if (more_items) request_first(next);
 
-            // ---- epilogue: through LDS (8 KB a wavefront in q stage 1, which is requested later), so that stores are whole lines.
-            // An MFMA result: lane l holds row l % 16 of its fragment and features 4 * (l / 16) + 0 .. 3.
-            unsigned char* own = lds + kQBase + kStage + wave * 8192;
+            // ---- epilogue: through LDS (8 KB a wavefront in the third stage of p, which is requested later), so that stores are whole lines.
+            // An MFMA result: lane l holds row l % 16 of its fragment and features 4 * (l / 16) + 0 .. 3.  Every store is issued, whether its rows
+            // exist or not (what does not lies behind the end of the buffer), so that wait_first() can count them.
+            unsigned char* own = lds + 2 * kStage + wave * 8192;
             if (!OUT32 && cur.piece < 0) {
                 // [16 rows][128 features] bf16, rows of 256 bytes, 16-byte unit u of row r at u ^ r
                 const int f = cur.f0 + wq * 128 + frow * 8;
-                uint16_t* out = static_cast<uint16_t*>(a.out) + (FORM == kWgrad ? (size_t)cur.expert * N * K : (size_t)0) + (size_t)cur.row0 * features + f;
+                const uint32_t stride = (uint32_t)features * 2u;
+                const __amdgpu_buffer_rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(
+                    static_cast<uint16_t*>(a.out) + (FORM == kWgrad ? (size_t)cur.expert * N * K : (size_t)0) + (size_t)cur.row0 * features, 0,
+                    (int)((uint32_t)cur.rows * stride), 0x00020000);
+                const uint32_t to = f < features ? (uint32_t)(wt * 16 + fpiece) * stride + (uint32_t)f * 2u : kNowhere;
 #pragma unroll
                 for (int i = 0; i < TFE; ++i) {
                     __builtin_amdgcn_sched_barrier(0);  // one fragment's values in registers at a time
@@ -281,21 +293,33 @@ struct TileKernel {
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
                         const int lr = h * 4 + fpiece;
-                        const int row = (2 * i + wt) * 16 + lr;
                         const u32x4 v = *reinterpret_cast<const u32x4*>(own + lr * 256 + ((frow ^ lr) << 4));
-                        if (row < cur.rows && f < features) *reinterpret_cast<u32x4*>(out + (size_t)row * features) = v;
+                        __builtin_amdgcn_raw_buffer_store_b128(v, out, to + (uint32_t)(i * 32 + h * 4) * stride, 0, kStreamed);
                     }
                     gg::wave_order();
                 }
+                stores = 4 * TFE;
             } else {
                 // [16 rows][128 features] fp32, rows of 512 bytes, 16-byte unit u of row r at u ^ r
                 const int unit = lane & 31, col = wq * 128 + unit * 4;
                 const bool piece = cur.piece >= 0;
-                float* out = piece ? scratch + (size_t)cur.piece * piece_units * kUnitFloats + col
-                                   : static_cast<float*>(a.out) + (size_t)cur.expert * N * K + (size_t)cur.row0 * features + cur.f0 + col;
-                const size_t stride = piece ? kTile : features;
-                const bool stores = cur.f0 + col < features;
+                const uint32_t stride = (uint32_t)(piece ? kTile : features) * 4u;
+                float* const tile_out = piece ? scratch + (size_t)cur.piece * piece_units * kUnitFloats
+                                              : static_cast<float*>(a.out) + (size_t)cur.expert * N * K + (size_t)cur.row0 * features + cur.f0;
+                // (the last row of a ragged feature tile ends before the next tile's memory)
+                const uint32_t bytes = (uint32_t)cur.rows * stride - (piece ? 0u : (uint32_t)cur.f0 * 4u);
+                const __amdgpu_buffer_rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(tile_out, 0, (int)bytes, 0x00020000);
+                const uint32_t to = cur.f0 + col < features ? (uint32_t)(wt * 16 + (lane >> 5)) * stride + (uint32_t)col * 4u : kNowhere;
                 const bool adds = OUT32 && !piece && a.accumulate;
+                u32x4 old[OUT32 ? 2 : 1][8];   // what is there already, two fragments ahead
+                auto fetch = [&](int i) GG_LAMBDA {
+#pragma unroll
+                    for (int h = 0; h < 8; ++h) old[OUT32 ? i % 2 : 0][h] = __builtin_amdgcn_raw_buffer_load_b128(out, to + (uint32_t)(i * 32 + h * 2) * stride, 0, kStreamed);
+                };
+                if (adds) {
+                    fetch(0);
+                    if (TFE > 1) fetch(1);
+                }
 #pragma unroll
                 for (int i = 0; i < TFE; ++i) {
                     __builtin_amdgcn_sched_barrier(0);
@@ -307,19 +331,23 @@ struct TileKernel {
                         *reinterpret_cast<f32x4*>(own + frow * 512 + (((j * 4 + fpiece) ^ frow) << 4)) = v;
                     }
                     gg::wave_order();
+                    f32x4 v[8];
 #pragma unroll
                     for (int h = 0; h < 8; ++h) {
                         const int lr = h * 2 + (lane >> 5);
-                        const int row = (2 * i + wt) * 16 + lr;
-                        f32x4 v = *reinterpret_cast<const f32x4*>(own + lr * 512 + ((unit ^ lr) << 4));
-                        if (row < cur.rows && stores) {
-                            f32x4* to = reinterpret_cast<f32x4*>(out + (size_t)row * stride);
-                            if (adds) v += *to;
-                            *to = v;
-                        }
+                        v[h] = *reinterpret_cast<const f32x4*>(own + lr * 512 + ((unit ^ lr) << 4));
                     }
+                    if (adds) {
+#pragma unroll
+                        for (int h = 0; h < 8; ++h) v[h] += __builtin_bit_cast(f32x4, old[OUT32 ? i % 2 : 0][h]);
+                        if (i + 2 < TFE) fetch(i + 2);
+                    }
+#pragma unroll
+                    for (int h = 0; h < 8; ++h)
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v[h]), out, to + (uint32_t)(i * 32 + h * 2) * stride, 0, kStreamed);
                     gg::wave_order();
                 }
+                stores = 8 * TFE;
             }
         };
         const int groups = uniform((cur.rows + 31) / 32);
@@ -344,6 +372,7 @@ struct TileKernel {
         }
         if (!more_items) break;
         cur = next;
+        gg::lds_barrier();   // (the results went through the stage that is requested next)
         }
     }
 };

@@ -69,12 +69,6 @@ struct Fp8Kernel {
             off[n] = (uint32_t)row * (uint32_t)K + (uint32_t)gg::swizzled(row, lane0 & 7) * 16u;
         }
         const uint32_t s_off = wave < 4 || (wave == 4 && lane0 < 2) ? (uint32_t)((wave & 3) * 64 + lane0) * (uint32_t)kb * 4u : kNowhere;
-        // Steps behind the last one read zeros: a buffer's end moves to its beginning.
-        auto advance = [](Buffer& b, uint32_t bytes, int steps_left) GG_LAMBDA {
-            if (steps_left <= 1) b.left = 0;
-            b.advance(bytes);
-        };
-        int p_steps, q_steps;   // that are still to be requested
         auto p_load = [&](uint32_t stage, int n) GG_LAMBDA {
             set_lds_target(wave_lds + stage * kPStage + n * 8192);
             load16(p.d, off[n]);
@@ -87,10 +81,10 @@ struct Fp8Kernel {
             set_lds_target(lds0 + kSBase + stage * kSStage + (uint32_t)wave * 256);
             load4(s.d, s_off);
         };
-        auto p_done = [&]() GG_LAMBDA { advance(p, kStepC, p_steps--); };
+        auto p_done = [&]() GG_LAMBDA { p.next_rows(kStepC); };
         auto q_done = [&]() GG_LAMBDA {
-            advance(q, kStepC, q_steps);
-            advance(s, 4, q_steps--);
+            q.next_rows(kStepC);
+            s.next_rows(4);
         };
         auto p_stage = [&](uint32_t stage) GG_LAMBDA {
 #pragma unroll
@@ -109,12 +103,11 @@ struct Fp8Kernel {
             const int block = t.c0 / kStepC;
             const uint8_t *pm = static_cast<const uint8_t*>(a.p), *qm = static_cast<const uint8_t*>(a.q);
             const int64_t at = (int64_t)t.f0 * K + t.c0;   // in the expert's matrix
-            p.set(pm + (size_t)t.expert * N * K + at, (int64_t)N * K - at);
-            q.set(qm + (size_t)t.row0 * K + t.c0, (int64_t)t.rows * K - t.c0);
+            p.set_rows(pm + (size_t)t.expert * N * K + at, (int64_t)min(kTile, N - t.f0) * K - t.c0, t.k_steps);
+            q.set_rows(qm + (size_t)t.row0 * K + t.c0, (int64_t)t.rows * K - t.c0, t.k_steps);
             const int f_block = t.f0 / 128;
             const float* sm = wave < 4 ? a.q_scales + (size_t)t.row0 * kb : a.p_scales + ((size_t)t.expert * nb + f_block) * kb;
-            s.set(sm + block, ((int64_t)(wave < 4 ? t.rows : nb - f_block) * kb - block) * 4);
-            p_steps = q_steps = t.k_steps;
+            s.set_rows(sm + block, ((int64_t)(wave < 4 ? t.rows : min(2, nb - f_block)) * kb - block) * 4, t.k_steps);
             q_stage(0, t.rows);
             p_stage(0);
             q_stage(1, t.rows);

@@ -274,31 +274,59 @@ struct Hand {
     }
 };
 
-// Memory from `p` on, `bytes` of it; what lies behind reads as zero.
+// A buffer descriptor of the memory from a K step of an operand on.  What lies behind its end reads as zero, and behind the last step
+// everything does.
 struct Buffer {
-    uint64_t at;
-    int64_t left;
     u32x4 d;
-    __device__ GG_INLINE void describe() {
-        d[0] = (uint32_t)at;
-        d[1] = (uint32_t)(at >> 32) & 0xffffu;
-        d[2] = left < 0 ? 0u : left > 0xffffffffll ? 0xffffffffu : (uint32_t)left;
-    }
-    __device__ GG_INLINE void set(const void* p, int64_t bytes) {
-        at = reinterpret_cast<uint64_t>(p);
-        at = (uint64_t)(uint32_t)uniform((int)(at >> 32)) << 32 | (uint32_t)uniform((int)(uint32_t)at);
-        left = (int64_t)((uint64_t)(uint32_t)uniform((int)(bytes >> 32)) << 32 | (uint32_t)uniform((int)(uint32_t)bytes));
+    int steps;   // left, this one included
+    // COLUMNS: lines of `line` bytes, a line for each c, of which c_left are left; the operand begins `skipped` bytes into a line.
+    int c_left;
+    uint32_t line, skipped;
+
+    __device__ GG_INLINE void begin_at(const void* p, int k_steps) {
+        const uint64_t at = reinterpret_cast<uint64_t>(p);
+        d[0] = (uint32_t)uniform((int)(uint32_t)at);
+        d[1] = (uint32_t)uniform((int)((uint32_t)(at >> 32) & 0xffffu));
         d[3] = 0x00020000u;
-        describe();
-        asm volatile("s_nop 4" : "+s"(d)::"memory");   // (a scalar register that a vector instruction wrote, before a load reads it)
+        steps = uniform(k_steps);
     }
-    __device__ GG_INLINE void advance(uint32_t bytes) {
-        at += bytes;
-        left -= bytes;
-        describe();
+    __device__ GG_INLINE void settle() { asm volatile("s_nop 4" : "+s"(d)::"memory"); }   // (a load reads what a vector instruction wrote)
+    // Rows whose contraction is contiguous: `bytes` to the end of the last one (at most 256 rows of 4 MiB).
+    __device__ GG_INLINE void set_rows(const void* p, int64_t bytes, int k_steps) {
+        begin_at(p, k_steps);
+        d[2] = (uint32_t)uniform((int)bytes);
+        settle();
+    }
+    template <int STEP>
+    __device__ GG_INLINE void set_columns(const void* p, int c, uint32_t line_bytes, uint32_t skipped_bytes, int k_steps) {
+        begin_at(p, k_steps);
+        c_left = uniform(c);
+        line = line_bytes;
+        skipped = (uint32_t)uniform((int)skipped_bytes);
+        bound_columns<STEP>();
+        settle();
+    }
+    template <int STEP>
+    __device__ GG_INLINE void bound_columns() { d[2] = c_left > 0 ? (uint32_t)min(c_left, STEP) * line - skipped : 0u; }
+    __device__ GG_INLINE void move(uint32_t bytes) {
+        const uint64_t at = ((uint64_t)d[1] << 32 | d[0]) + bytes;   // (an address has 48 bits: nothing moves into the fields above)
+        d[0] = (uint32_t)at;
+        d[1] = (uint32_t)(at >> 32);
+    }
+    // On to the next K step.
+    __device__ GG_INLINE void next_rows(uint32_t bytes) {
+        move(bytes);
+        --steps;
+        d[2] = steps > 0 ? d[2] - bytes : 0u;
+    }
+    template <int STEP>
+    __device__ GG_INLINE void next_columns() {
+        move(STEP * line);
+        --steps;
+        c_left = steps > 0 ? c_left - STEP : 0;
+        bound_columns<STEP>();
     }
 };
-
 
 // Adds the pieces of the tiles that were cut: 32 rows of one of them for each workgroup.
 template <int FORM, int STEP, bool OUT32>
