@@ -12,7 +12,13 @@
 // tile of 256 x 192), two on a SIMD: 96 accumulators, the weights' fragments of this and the next K step and some of the rows' are the
 // 256 registers that each has, and one's MFMAs run under the other's additions.
 //
-// LDS: three stages of weights, whose lines come from memory, two of rows, three of scales (numbers of 192 rows and two blocks of weights).
+// LDS: three stages of weights, whose lines come from memory, two of rows, two of the scales of four K steps (of 192 rows and two blocks of
+// weights).  A row's scales are 16 bytes of a line of their own, which cost the load path as much as a whole line of operands: four K steps'
+// at a time they are a tenth of its work, one by one they were three tenths.
+//
+// What bounds it: MFMAs, additions and LDS reads alone run at 3.1 PFLOP/s, at 1.5 GHz on numbers with all their bits in use; with the lines
+// on their way to LDS as well it is 2.25 at 6144 x 6144 x 16384, 64 % of the cycles MFMAs at 1.7 GHz: the board is at its power limit, and what moves
+// data costs clock.  (A tile of 256 x 160, which leaves room for three stages of rows: 1.99 at 60 % and 1.62 GHz.)
 #include "products_tiles.h"
 
 namespace moe {
@@ -27,9 +33,9 @@ constexpr int kStepC = 128, kTallest = 192;
 struct Fp8Kernel {
     static constexpr int kThreads = 512;
     static constexpr int kF = 4;                       // fragments of 16 features a wavefront
-    static constexpr int kPStage = 32768, kQStage = kTallest * 128, kSStage = 2048;
+    static constexpr int kPStage = 32768, kQStage = kTallest * 128, kSStage = 4096;
     static constexpr uint32_t kQBase = 3 * kPStage, kSBase = kQBase + 2 * kQStage;
-    static constexpr int kLdsBytes = kSBase + 3 * kSStage;
+    static constexpr int kLdsBytes = kSBase + 2 * kSStage;
     static constexpr uint32_t kNowhere = 0xc0000000u;  // a lane offset behind the end of every buffer
     static constexpr int kLate = 3;                    // MFMAs between one and the addition of its result
 
@@ -37,7 +43,6 @@ struct Fp8Kernel {
 
     static __device__ GG_INLINE void set_lds_target(uint32_t a) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" ::"s"(a) : "memory"); }
     static __device__ GG_INLINE void load16(u32x4 d, uint32_t off) { asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(d) : "memory"); }
-    static __device__ GG_INLINE void load4(u32x4 d, uint32_t off) { asm volatile("buffer_load_dword %0, %1, 0 offen lds" ::"v"(off), "s"(d) : "memory"); }
     // d = the block's sum.  An asm statement keeps its place among the others and its result in VGPRs.  What the compiler does not know
     // is that it is an MFMA: a result is not touched for kLate MFMAs and the additions between them, 15 instructions (12 are
     // needed behind these eight passes), and settle() stands before the last ones; tests/test_products_isa.py reads the built kernel for it.
@@ -47,6 +52,23 @@ struct Fp8Kernel {
     // acc += d * by (an asm statement as well: the compiler moves additions away from the MFMA whose registers they free)
     static __device__ GG_INLINE void add_scaled(float& acc, float d, float by) { asm volatile("v_fmac_f32 %0, %1, %2" : "+v"(acc) : "v"(d), "v"(by)); }
     static __device__ GG_INLINE void settle() { asm volatile("s_nop 15" ::: "memory"); }
+
+    static constexpr int kStreamed = 2;   // cache policy of results: not kept in favour of operands
+    // Waits for the first two K steps of an item, which were requested before the `stores` of the item before.
+    static __device__ GG_INLINE void wait_first(int stores) {
+        switch (stores) {
+            case 0: gg::wait_vmcnt<0>(); break;
+            case 2: gg::wait_vmcnt<2>(); break;
+            case 4: gg::wait_vmcnt<4>(); break;
+            case 6: gg::wait_vmcnt<6>(); break;
+            case 8: gg::wait_vmcnt<8>(); break;
+            case 10: gg::wait_vmcnt<10>(); break;
+            case 12: gg::wait_vmcnt<12>(); break;
+            case 16: gg::wait_vmcnt<16>(); break;
+            case 20: gg::wait_vmcnt<20>(); break;
+            default: gg::wait_vmcnt<24>(); break;
+        }
+    }
 
     template <class Decode>
     static __device__ GG_INLINE void run(const Args& a, float* scratch, int piece_units, unsigned char* lds, Item cur, const Decode& decode) {
@@ -59,7 +81,7 @@ struct Fp8Kernel {
         auto next_of_3 = [](uint32_t s) GG_LAMBDA { return s == 2 ? 0u : s + 1; };
 
         // Load n of wavefront w covers rows n * 64 + w * 8 .. + 7, lane l the 16-byte piece that belongs at position l % 8 of row l / 8.
-        // Scales: wavefront w < 4 its 64 rows', wavefront 4 the weights' two, the others nothing (they load zeros, so that all wait alike).
+        // Scales: wavefronts 0 to 2 those of 64 rows each, 3 the weights' two.  (A load takes dwords at any dword's address, and checks each for the end.)
         uint32_t off[4];   // of both operands
         Buffer p, q, s;
         const int lane0 = threadIdx.x & 63;
@@ -68,7 +90,7 @@ struct Fp8Kernel {
             const int row = n * 64 + wave * 8 + (lane0 >> 3);
             off[n] = (uint32_t)row * (uint32_t)K + (uint32_t)gg::swizzled(row, lane0 & 7) * 16u;
         }
-        const uint32_t s_off = wave < 4 || (wave == 4 && lane0 < 2) ? (uint32_t)((wave & 3) * 64 + lane0) * (uint32_t)kb * 4u : kNowhere;
+        const uint32_t s_off = wave < 3 || lane0 < 2 ? (uint32_t)((wave < 3 ? wave * 64 : 0) + lane0) * (uint32_t)kb * 4u : kNowhere;
         auto p_load = [&](uint32_t stage, int n) GG_LAMBDA {
             set_lds_target(wave_lds + stage * kPStage + n * 8192);
             load16(p.d, off[n]);
@@ -77,26 +99,24 @@ struct Fp8Kernel {
             set_lds_target(wave_lds + kQBase + stage * kQStage + n * 8192);
             load16(q.d, off[n]);
         };
-        auto s_load = [&](uint32_t stage) GG_LAMBDA {
-            set_lds_target(lds0 + kSBase + stage * kSStage + (uint32_t)wave * 256);
-            load4(s.d, s_off);
+        auto s_load = [&](uint32_t stage) GG_LAMBDA {   // of the next four steps
+            if (wave >= 4) return;
+            set_lds_target(wave_lds + kSBase + stage * kSStage);
+            load16(s.d, s_off);
+            s.next_rows(16);
         };
-        auto p_done = [&]() GG_LAMBDA { p.next_rows(kStepC); };
-        auto q_done = [&]() GG_LAMBDA {
-            q.next_rows(kStepC);
-            s.next_rows(4);
-        };
+        auto p_next = [&]() GG_LAMBDA { p.next_rows(kStepC); };
+        auto q_next = [&]() GG_LAMBDA { q.next_rows(kStepC); };
         auto p_stage = [&](uint32_t stage) GG_LAMBDA {
 #pragma unroll
             for (int n = 0; n < 4; ++n) p_load(stage, n);
-            p_done();
+            p_next();
         };
-        auto q_stage = [&](uint32_t stage, int rows) GG_LAMBDA {   // with the scales
+        auto q_stage = [&](uint32_t stage, int rows) GG_LAMBDA {
 #pragma unroll
             for (int n = 0; n < 3; ++n)
                 if (n * 64 + wave * 8 < rows) q_load(stage, n);
-            s_load(stage);
-            q_done();
+            q_next();
         };
         // The first two steps of an item.
         auto request_first = [&](const Item& t) GG_LAMBDA {
@@ -106,29 +126,31 @@ struct Fp8Kernel {
             p.set_rows(pm + (size_t)t.expert * N * K + at, (int64_t)min(kTile, N - t.f0) * K - t.c0, t.k_steps);
             q.set_rows(qm + (size_t)t.row0 * K + t.c0, (int64_t)t.rows * K - t.c0, t.k_steps);
             const int f_block = t.f0 / 128;
-            const float* sm = wave < 4 ? a.q_scales + (size_t)t.row0 * kb : a.p_scales + ((size_t)t.expert * nb + f_block) * kb;
-            s.set_rows(sm + block, ((int64_t)(wave < 4 ? t.rows : min(2, nb - f_block)) * kb - block) * 4, t.k_steps);
+            const float* sm = wave < 3 ? a.q_scales + (size_t)t.row0 * kb : a.p_scales + ((size_t)t.expert * nb + f_block) * kb;
+            s.set_rows(sm + block, ((int64_t)(wave < 3 ? t.rows : min(2, nb - f_block)) * kb - block) * 4, (t.k_steps + 3) / 4);
+            s_load(0);
             q_stage(0, t.rows);
             p_stage(0);
             q_stage(1, t.rows);
             p_stage(1);
         };
 
+        int stores = 0;   // of the item before
         request_first(cur);
         for (int n = 1;; ++n) {
         int tid = threadIdx.x;   // (opaque: lane addresses are computed where they are used)
         asm volatile("" : "+v"(tid));
         const int lane = tid & 63;
+        wait_first(stores);
+        gg::lds_barrier();   // (the results of the item before went through the third stage, too)
         p_stage(2);
-        gg::wait_vmcnt<4>();     // all but the four loads of that
-        gg::lds_barrier();
 
         // Fragments: 16 rows x 128 bytes.  Lane l holds row l % 16, pieces l / 16 and l / 16 + 4 (any 32 bytes of the block do, if both operands
         // take the same), at r * 128 + ((piece ^ ((r >> 1) & 7)) << 4).  Feature fragment j: features wq * 64 + j * 16; row fragment i: rows (2 i + wt) * 16.
         const int frow = lane & 15, fpiece = lane >> 4;
         const uint32_t in_row = (uint32_t)(frow * 128 + ((((frow >> 1) & 7) ^ fpiece) << 4));
         const uint32_t p_read = (uint32_t)(wq * 64) * 128 + in_row, q_read = kQBase + (uint32_t)wt * 2048 + in_row;
-        const uint32_t x_read = kSBase + (uint32_t)(wt * 16 + frow) * 4, w_read = kSBase + 1024 + (uint32_t)(wq >> 1) * 4;
+        const uint32_t x_read = kSBase + (uint32_t)(wt * 16 + frow) * 16, w_read = kSBase + 3072 + (uint32_t)(wq >> 1) * 16;
         auto fragment = [&](uint32_t at, int rows) GG_LAMBDA {
             typedef __attribute__((address_space(3))) const i32x4* piece;
             const i32x4 lo = *reinterpret_cast<piece>(lds3 + at + rows * 128), hi = *reinterpret_cast<piece>(lds3 + (at ^ 64u) + rows * 128);
@@ -175,21 +197,25 @@ struct Fp8Kernel {
             float by[TFE], by_before = 0.f;   // scales of the rows times those of the weights; of the last rows in the step before
             // Step kt: its MFMAs out of fragment buffer B, between them the reads of what is left of the step's rows, then, when step kt + 1 is there,
             // of its weights and first rows, and the requests of the rows and scales of kt + 2 and of the weights of kt + 3.
-            uint32_t p_at = 0, q_at = 0, s_at = 0;   // stages of step kt
+            uint32_t p_at = 0, q_at = 0, s_at = 0;   // stages of step kt; where its scales are behind those of step 0
             auto k_step = [&](auto buf) GG_LAMBDA {
                 constexpr int B = decltype(buf)::value;
-                const uint32_t p1 = next_of_3(p_at), q1 = q_at ^ 1, s1 = next_of_3(s_at), s2 = next_of_3(s1);
-                constexpr int kLoads = (TFE + 1) / 2 + 1 + kF, kRest = kM - kTurn;
+                const uint32_t p1 = next_of_3(p_at), q1 = q_at ^ 1;
+                // four steps in a stage of scales
+                const uint32_t s1 = B == 0 ? s_at + 4 : (s_at & 12) == 12 ? (s_at ^ kSStage) - 12 : s_at + 4;
+                constexpr int kRowLoads = (TFE + 1) / 2, kLoads = kRowLoads + kF, kRest = kM - kTurn;
 #pragma unroll
                 for (int m = 0; m < kM; ++m) {
                     if (m == kTurn) {
-                        // Outstanding, oldest first: rows, scales and weights of kt + 1 (the latter requested a step before), weights of kt + 2 (four loads).
-                        gg::wait_vmcnt<4>();
+                        // Outstanding, oldest first: weights of kt + 1, rows and scales of kt + 1, weights of kt + 2 (four loads).  At step 0 the stores of
+                        // the item before come ahead of the last ones, and what is needed is there already.
+                        if (left < cur.k_steps) gg::wait_vmcnt<4>();
                         gg::lds_barrier();
                         if (ragged && left == 2) clear_second_halves(p1, q1);
                     }
                     block_sum(d[m % (kLate + 1)], pf[B][m % kF], qf[B][m / kF]);
-                    if (m % kF == 0) by[m / kF] = xs[B][m / kF] * ws[B];
+                    // (behind the last step there may be another row's scale, and zero times that need not be zero)
+                    if (m % kF == 0) by[m / kF] = B == 0 || left > 0 ? xs[B][m / kF] * ws[B] : 0.f;
                     if (m >= kLate) add(m - kLate, by[(m - kLate) / kF]);
                     else add(m - kLate + kM, by_before);
                     if (m < kTurn) {
@@ -197,7 +223,7 @@ struct Fp8Kernel {
                         for (int x = 0; x < kFirst; ++x)
                             if (x * kTurn / (kFirst > 0 ? kFirst : 1) == m) {
                                 qf[B][kHeld + x] = fragment(q_read + q_at * kQStage, (kHeld + x) * 32);
-                                xs[B][kHeld + x] = number(x_read + s_at * kSStage + (kHeld + x) * 128);
+                                xs[B][kHeld + x] = number(x_read + s_at + (kHeld + x) * 512);
                             }
                     } else {
 #pragma unroll
@@ -207,20 +233,18 @@ struct Fp8Kernel {
                                 pf[1 - B][x] = fragment(p_read + p1 * kPStage, x * 16);
                             } else {
                                 qf[1 - B][x - kF] = fragment(q_read + q1 * kQStage, (x - kF) * 32);
-                                xs[1 - B][x - kF] = number(x_read + s1 * kSStage + (x - kF) * 128);
-                                if (x == kF) ws[1 - B] = number(w_read + s1 * kSStage);
+                                xs[1 - B][x - kF] = number(x_read + s1 + (x - kF) * 512);
+                                if (x == kF) ws[1 - B] = number(w_read + s1);
                             }
                         }
 #pragma unroll
                         for (int x = 0; x < kLoads; ++x) {
                             if (kTurn + x * kRest / kLoads != m) continue;
-                            constexpr int kRowLoads = (TFE + 1) / 2;
                             if (x < kRowLoads) {
                                 if (x * 2 + 2 <= TFE || wave < 4) q_load(q_at, x);   // 64 rows, or the last 32
-                            } else if (x == kRowLoads) {
-                                s_load(s2);
                             } else {
-                                p_load(p_at, x - kRowLoads - 1);
+                                if (B == 0 && x == kRowLoads && (s_at & 12) == 0) s_load(s_at == 0 ? 1u : 0u);
+                                p_load(p_at, x - kRowLoads);
                             }
                         }
                     }
@@ -228,8 +252,8 @@ struct Fp8Kernel {
                 }
                 by_before = by[TFE - 1];   // (the last MFMAs of this step are added in the next)
                 --left;
-                q_done();
-                p_done();
+                q_next();
+                p_next();
                 p_at = p1;
                 q_at = q1;
                 s_at = s1;
@@ -241,7 +265,7 @@ struct Fp8Kernel {
 #pragma unroll
             for (int i = 0; i < kHeld; ++i) {
                 qf[0][i] = fragment(q_read, i * 32);
-                xs[0][i] = number(x_read + i * 128);
+                xs[0][i] = number(x_read + i * 512);
             }
             ws[0] = number(w_read);
             do {   // (two steps at a time, for the two fragment buffers; a step behind the last one adds zeros)
@@ -258,12 +282,16 @@ struct Fp8Kernel {
             gg::lds_barrier();   // every wavefront is done reading operand tiles; no load is outstanding
             if (more_items) request_first(next);
 
-            // ---- epilogue: through LDS (4 KB a wavefront in the third stage of weights, which is requested later), so that stores are whole lines
+            // ---- epilogue: through LDS (4 KB a wavefront in the third stage of weights, which is requested later), so that stores are whole lines.
+            // Every store is issued (what does not exist lies behind the end of the buffer), so that wait_first() can count them.
             unsigned char* own = lds + 2 * kPStage + wave * 4096;
             if (cur.piece < 0) {
                 // [16 rows][64 features] bf16, rows of 128 bytes, 16-byte unit u of row r at swizzled(r, u)
                 const int f = cur.f0 + wq * 64 + (lane & 7) * 8;
-                uint16_t* out = static_cast<uint16_t*>(a.out) + (size_t)cur.row0 * N + f;
+                const uint32_t stride = (uint32_t)N * 2u;
+                const __amdgpu_buffer_rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(static_cast<uint16_t*>(a.out) + (size_t)cur.row0 * N, 0,
+                                                                                    (int)((uint32_t)cur.rows * stride), 0x00020000);
+                const uint32_t to = f < N ? (uint32_t)(wt * 16 + (lane >> 3)) * stride + (uint32_t)f * 2u : kNowhere;
 #pragma unroll
                 for (int i = 0; i < TFE; ++i) {
 #pragma unroll
@@ -275,30 +303,33 @@ struct Fp8Kernel {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int lr = h * 8 + (lane >> 3);
-                        const int row = (2 * i + wt) * 16 + lr;
                         const u32x4 v = *reinterpret_cast<const u32x4*>(own + lr * 128 + gg::swizzled(lr, lane & 7) * 16);
-                        if (row < cur.rows && f < N) *reinterpret_cast<u32x4*>(out + (size_t)row * N) = v;
+                        __builtin_amdgcn_raw_buffer_store_b128(v, out, to + (uint32_t)(i * 32 + h * 8) * stride, 0, kStreamed);
                     }
                     gg::wave_order();
                 }
+                stores = 2 * TFE;
             } else {
                 // [16 rows][64 features] fp32, rows of 256 bytes, 16-byte unit u of row r at u ^ r
                 const int col = wq * 64 + frow * 4;
-                float* out = scratch + (size_t)cur.piece * piece_units * kUnitFloats + col;
+                const __amdgpu_buffer_rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(scratch + (size_t)cur.piece * piece_units * kUnitFloats, 0,
+                                                                                    cur.rows * kTile * 4, 0x00020000);
+                const uint32_t to = cur.f0 + col < N ? (uint32_t)((wt * 16 + fpiece) * kTile + col) * 4u : kNowhere;
 #pragma unroll
                 for (int i = 0; i < TFE; ++i) {
 #pragma unroll
-                    for (int j = 0; j < kF; ++j) *reinterpret_cast<f32x4*>(own + frow * 256 + (((j * 4 + fpiece) ^ frow) << 4)) = f32x4{acc[j][i][0], acc[j][i][1], acc[j][i][2], acc[j][i][3]};
+                    for (int j = 0; j < kF; ++j)
+                        *reinterpret_cast<f32x4*>(own + frow * 256 + (((j * 4 + fpiece) ^ frow) << 4)) = f32x4{acc[j][i][0], acc[j][i][1], acc[j][i][2], acc[j][i][3]};
                     gg::wave_order();
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
                         const int lr = h * 4 + fpiece;
-                        const int row = (2 * i + wt) * 16 + lr;
-                        const f32x4 v = *reinterpret_cast<const f32x4*>(own + lr * 256 + ((frow ^ lr) << 4));
-                        if (row < cur.rows && cur.f0 + col < N) *reinterpret_cast<f32x4*>(out + (size_t)row * kTile) = v;
+                        const u32x4 v = *reinterpret_cast<const u32x4*>(own + lr * 256 + ((frow ^ lr) << 4));
+                        __builtin_amdgcn_raw_buffer_store_b128(v, out, to + (uint32_t)((i * 32 + h * 4) * kTile) * 4u, 0, 0);
                     }
                     gg::wave_order();
                 }
+                stores = 4 * TFE;
             }
         };
         switch (uniform((cur.rows + 31) / 32)) {
@@ -311,7 +342,6 @@ struct Fp8Kernel {
         }
         if (!more_items) break;
         cur = next;
-        gg::lds_barrier();   // (the results went through the stage that is requested next)
         }
     }
 };
@@ -319,7 +349,7 @@ struct Fp8Kernel {
 __global__ __launch_bounds__(Fp8Kernel::kThreads, 1) void product_fp8_kernel(Args a, float* scratch, Plan* told) {
     __shared__ __attribute__((aligned(1024))) unsigned char lds[Fp8Kernel::kLdsBytes];
     Tiles<kForward, kStepC> list(a);
-    const Plan plan = choose_tiles(list, a.n, gridDim.x, {kTallest, 60, 8});
+    const Plan plan = choose_tiles(list, a.n, gridDim.x, {kTallest, 60, 13});
     list.build(plan.height);
     if (blockIdx.x == 0 && threadIdx.x == 0) *told = plan;
     const Items<kForward, kStepC> items(list, plan);
