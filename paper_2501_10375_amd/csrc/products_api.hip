@@ -53,7 +53,7 @@ int enqueue(products::Form form, const moe_product_t& p, int32_t rows, const voi
     const Args a = {q, second, out, offsets, p.n_experts, rows, p.out_features, p.in_features, nullptr, nullptr, accumulate};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (form == products::kForward && p.dtype == MOE_BF16 && products::few_rows(a, false)) return status(products::launch_few_rows(a, false, stream));
-    return status(p.dtype == MOE_F32 ? products::launch_f32(form, a, stream) : products::launch_bf16(form, a, out_f32, workspace, stream));
+    return status(p.dtype == MOE_F32 ? products::launch_f32(form, a, workspace, stream) : products::launch_bf16(form, a, out_f32, workspace, stream));
 }
 
 }  // namespace

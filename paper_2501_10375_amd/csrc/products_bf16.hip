@@ -27,7 +27,7 @@ hipError_t launch_bf16(Form form, const Args& a, bool out_f32, void* workspace, 
     }
 }
 
-size_t product_workspace_bytes(const moe_product_t& p, int) { return p.dtype == MOE_F32 ? 256 : kScratchBytes + 256; }
+size_t product_workspace_bytes(const moe_product_t& p, int) { return p.dtype == MOE_F32 ? kScratchFloats * sizeof(float) : kScratchBytes + 256; }
 
 }  // namespace products
 }  // namespace moe

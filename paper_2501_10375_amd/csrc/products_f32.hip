@@ -1,12 +1,18 @@
 // Grouped products on the fp32 matrix instructions: the forward product and both gradients of one tile kernel.
 //
-// A workgroup computes a square tile of the output, its four wavefronts a quarter each.  Every K step of 16 goes through LDS as
-// [c][row] for both operands, whichever way they lie in memory: an operand whose contraction is contiguous is written transposed,
-// one whose rows are (the weights of dgrad, both operands of wgrad) as it is.  v_mfma_f32_16x16x4_f32 takes one number a lane,
-// row lane % 16 and c lane / 16, so a fragment is one ds_read_b32 without bank conflicts (a row of the LDS is the tile + 16 floats,
-// 16 banks further than the one before).  The features are the instruction's first operand, so that a lane ends
-// up with four consecutive ones of a row.
-#include "bf16_utils.h"
+// A workgroup computes 64 features of up to 64 rows, its four wavefronts a quarter each (of 16 rows: 16 features each).  Every K step
+// of 16 goes through LDS as [c][row] for both operands, whichever way they lie in memory: an operand whose contraction is contiguous is
+// written transposed, one whose rows are (the weights of dgrad, both operands of wgrad) as it is.  v_mfma_f32_16x16x4_f32 takes one number a
+// lane, row lane % 16 and c lane / 16, so a fragment is one ds_read_b32 without bank conflicts (a row of the LDS is the tile + 16 floats,
+// 16 banks further than the one before).  The features are the instruction's first operand, so that a lane ends up with four
+// consecutive ones of a row.
+//
+// Large products are bound by the MFMAs (4096^3: 116 of the 150 TFLOP/s that a library product reaches), with few rows by the weights (64 rows, 8 experts
+// of 4096 x 4096: 139 us forward, 106 dgrad, 5.1 TB/s), small ones by the time that a K step takes from its loads to its last MFMA, which
+// other workgroups of a CU have to fill: where there are few, the contraction is cut and a second kernel adds the parts (8 rows of 1024 x 1024: 40 ->
+// 13 us).
+#include <type_traits>
+
 #include "products_internal.h"
 
 namespace moe {
@@ -14,182 +20,221 @@ namespace products {
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(2))) float f32x2;
 
-constexpr int kThreads = 256, kBK = 16;
+constexpr int kThreads = 256, kBK = 16, kTileF = 64;
+constexpr long kMostWorkgroups = 2048;
+constexpr int kAhead = 4;   // K steps requested ahead
+
+__host__ __device__ inline size_t output_size(int form, const Args& a) {
+    return form == kWgrad ? (size_t)a.experts * a.n * a.k : (size_t)a.rows * (form == kForward ? a.n : a.k);
+}
 
 __device__ inline f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
-__device__ inline f32x4 load4(const uint16_t* p) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
-    return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)};
-}
-__device__ inline f32x4 load4(const uint8_t* p) {
-    const int v = *reinterpret_cast<const int*>(p);
-    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(v, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(v, true);
-    return f32x4{a[0], a[1], b[0], b[1]};
-}
 __device__ inline void store4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
-__device__ inline void store4(uint16_t* p, f32x4 v) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-}
 
-// One operand of a tile: `base` is its element (row 0, c 0).  ROWS: the contraction is contiguous, consecutive rows are `ld` apart; else
-// rows are contiguous and consecutive c are `ld` apart.  Rows from `limit` on don't exist, nor do c from `depth` on.
-template <typename T, bool ROWS, int TILE>
+// One operand of a tile.  ROWS: the contraction is contiguous, consecutive rows are `ld` apart; else rows are contiguous and consecutive c are
+// `ld` apart.  CUT: the contraction may end inside a K step (the rows of an expert); c from `depth` on count as zeros.
+template <bool ROWS, int TILE, bool CUT>
 struct Operand {
-    static constexpr int kQuads = TILE * kBK / 4 / kThreads;
-    const T* base;
-    size_t ld;
-    int limit, depth;
-    const float* scales;   // per row of the tile (ROWS), or a single one; null: none
-    size_t scale_ld;
-    f32x4 v[kQuads];
+    static constexpr int kAll = TILE * kBK / 4;   // four numbers a thread, or less
+    static_assert(kAll <= kThreads, "");
+    const float* at;   // this thread's four numbers of the next K step that is requested
+    size_t step;
+    int c_left;        // CUT: c from them to the end
+    f32x4 v[kAhead];   // K steps on their way
 
-    __device__ void load(int c0) {
-#pragma unroll
-        for (int i = 0; i < kQuads; ++i) {
-            const int t = threadIdx.x + i * kThreads;
-            const int row = ROWS ? t / 4 : t % (TILE / 4) * 4, c = c0 + (ROWS ? t % 4 * 4 : t / (TILE / 4));
-            v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (row < limit && c < depth) {
-                v[i] = load4(base + (ROWS ? (size_t)row * ld + c : (size_t)c * ld + row));
-                if constexpr (sizeof(T) == 1) v[i] *= scales[row * scale_ld + c / 128];
-            }
-        }
+    // `base`: element (row 0, c 0) of the tile, of which `limit` rows exist (rows behind them repeat the last one), begin: first c.
+    __device__ void set(const float* base, size_t ld, int limit, int begin, int depth) {
+        const int t = threadIdx.x;
+        const int row = ROWS ? min(t / 4, limit - 1) : t % (TILE / 4) * 4, c = begin + (ROWS ? t % 4 * 4 : t / (TILE / 4));
+        at = base + (ROWS ? (size_t)row * ld + c : (size_t)c * ld + row);
+        step = ROWS ? kBK : kBK * ld;
+        c_left = depth - c;
     }
+    template <int SLOT>
+    __device__ void load() {
+        v[SLOT] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if ((!CUT || c_left > 0) && (kAll == kThreads || threadIdx.x < kAll)) v[SLOT] = load4(at);
+        at += step;
+        if (CUT) c_left -= kBK;
+    }
+    template <int SLOT>
     __device__ void stage(float* lds) const {
+        const int t = threadIdx.x;
+        if (kAll < kThreads && t >= kAll) return;
+        if constexpr (ROWS) {
 #pragma unroll
-        for (int i = 0; i < kQuads; ++i) {
-            const int t = threadIdx.x + i * kThreads;
-            if constexpr (ROWS) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) lds[(t % 4 * 4 + j) * (TILE + 16) + t / 4] = v[i][j];
-            } else {
-                *reinterpret_cast<f32x4*>(lds + t / (TILE / 4) * (TILE + 16) + t % (TILE / 4) * 4) = v[i];
-            }
+            for (int j = 0; j < 4; ++j) lds[(t % 4 * 4 + j) * (TILE + 16) + t / 4] = v[SLOT][j];
+        } else {
+            *reinterpret_cast<f32x4*>(lds + t / (TILE / 4) * (TILE + 16) + t % (TILE / 4) * 4) = v[SLOT];
         }
     }
 };
 
-template <typename T, typename O, int FORM, int TILE>
-__global__ __launch_bounds__(kThreads, 2) void product_kernel(Args a) {
-    constexpr int kF = TILE / 32;   // fragments of each operand a wavefront
-    __shared__ __attribute__((aligned(16))) float lds[2][2][kBK * (TILE + 16)];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// HEIGHT: rows of a tile, 64 or 16.  With `parts` > 1 workgroup (x, s) adds up part s of the contraction and stores it as part s of the scratch memory,
+// laid out like the output.
+template <int FORM, int HEIGHT>
+__global__ __launch_bounds__(kThreads, 2) void product_kernel(Args a, int parts, float* scratch) {
+    constexpr int kAcross = HEIGHT == 64 ? 2 : 4;          // wavefronts across the features
+    constexpr int kP = kTileF / 16 / kAcross, kQ = HEIGHT / 16 / (4 / kAcross);   // fragments of a wavefront
+    constexpr int kPLd = kTileF + 16, kQLd = HEIGHT + 16;
+    __shared__ __attribute__((aligned(16))) float lds[2][kBK * (kPLd + kQLd)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int features = FORM == kForward ? a.n : a.k;
-    const int f_tiles = (features + TILE - 1) / TILE;
-    const int f0 = blockIdx.x % f_tiles * TILE;
+    const int f_tiles = features / kTileF;
+    const int f0 = blockIdx.x % f_tiles * kTileF;
     const int m = blockIdx.x / f_tiles;
     int e, row0, rows, depth;
-    Operand<T, FORM == kForward, TILE> p;
-    Operand<T, FORM != kWgrad, TILE> q;
-    O* out;
+    Operand<FORM == kForward, kTileF, FORM == kWgrad> p;
+    Operand<FORM != kWgrad, HEIGHT, FORM == kWgrad> q;
+    const float *p_base, *q_base;
+    size_t q_ld, out_at;
     if constexpr (FORM == kWgrad) {
-        const int n_tiles = (a.n + TILE - 1) / TILE;
+        const int n_tiles = a.n / HEIGHT;
         e = m / n_tiles;
-        const int n0 = m % n_tiles * TILE;
+        const int n0 = m % n_tiles * HEIGHT;
         int first, end;
         expert_rows(a, lane, first, end);
         first = __builtin_amdgcn_readlane(first, e);
         depth = __builtin_amdgcn_readlane(end, e) - first;
-        rows = min(TILE, a.n - n0);
-        q.base = static_cast<const T*>(a.q) + (size_t)first * a.n + n0;
-        q.ld = a.n;
-        p.base = static_cast<const T*>(a.p) + (size_t)first * a.k + f0;
-        p.ld = a.k;
-        out = static_cast<O*>(a.out) + ((size_t)e * a.n + n0) * a.k + f0;
+        if (depth == 0 && a.accumulate) return;   // (such an expert's gradient stays as it is; the parts of it are not read)
+        rows = HEIGHT;
+        q_base = static_cast<const float*>(a.q) + (size_t)first * a.n + n0;
+        q_ld = a.n;
+        p_base = static_cast<const float*>(a.p) + (size_t)first * a.k + f0;
+        out_at = ((size_t)e * a.n + n0) * a.k + f0;
     } else {
-        if (!find_row_tile(a, m, TILE, e, row0, rows)) return;
+        if (!find_row_tile(a, m, HEIGHT, e, row0, rows)) return;
         depth = FORM == kForward ? a.k : a.n;
-        q.base = static_cast<const T*>(a.q) + (size_t)row0 * depth;
-        q.ld = depth;
-        p.base = static_cast<const T*>(a.p) + (size_t)e * a.n * a.k + (FORM == kForward ? (size_t)f0 * a.k : f0);
-        p.ld = a.k;
-        out = static_cast<O*>(a.out) + (size_t)row0 * features + f0;
-        if constexpr (sizeof(T) == 1) {
-            const int kb = (a.k + 127) / 128, nb = (a.n + 127) / 128;
-            q.scales = a.q_scales + (size_t)row0 * kb;
-            q.scale_ld = kb;
-            p.scales = a.p_scales + ((size_t)e * nb + f0 / 128) * kb;
-            p.scale_ld = 0;
-        }
+        q_base = static_cast<const float*>(a.q) + (size_t)row0 * depth;
+        q_ld = depth;
+        p_base = static_cast<const float*>(a.p) + (size_t)e * a.n * a.k + (FORM == kForward ? (size_t)f0 * a.k : f0);
+        out_at = (size_t)row0 * features + f0;
     }
-    q.limit = rows;
-    p.limit = min(TILE, features - f0);
-    q.depth = p.depth = depth;
-
-    const int wf = wave % 2 * (TILE / 2), wr = wave / 2 * (TILE / 2);   // this wavefront's quarter
-    const int at = lane / 16 * (TILE + 16) + lane % 16;
-    f32x4 acc[kF][kF];   // [feature fragment][row fragment]
+    // This wavefront's part of the tile: row fragments wr, wr + 2 ..., so that a ragged tile's are shared out evenly.
+    constexpr int kDown = 4 / kAcross;
+    const int wf = wave % kAcross * (16 * kP), wr = wave / kAcross;
+    const int at_p = lane / 16 * kPLd + lane % 16 + wf, at_q = lane / 16 * kQLd + lane % 16 + wr * 16;
+    const int fragments = min(kQ, ((rows + 15) / 16 - wr + kDown - 1) / kDown);   // of rows that exist
+    f32x4 acc[kP][kQ];   // [feature fragment][row fragment]
 #pragma unroll
-    for (int i = 0; i < kF; ++i)
+    for (int i = 0; i < kP; ++i)
 #pragma unroll
-        for (int j = 0; j < kF; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int steps = (depth + kBK - 1) / kBK;
-    if (steps > 0) {
-        p.load(0);
-        q.load(0);
-    }
-    for (int s = 0; s < steps; ++s) {
-        float *lp = lds[s & 1][0], *lq = lds[s & 1][1];
-        p.stage(lp);
-        q.stage(lq);
+        for (int j = 0; j < kQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int all = (depth + kBK - 1) / kBK;
+    const int begin = (int)((long)all * blockIdx.y / parts), steps = (int)((long)all * (blockIdx.y + 1) / parts);
+    p.set(p_base, a.k, kTileF, begin * kBK, depth);
+    q.set(q_base, q_ld, rows, begin * kBK, depth);
+    auto request = [&](auto slot, int s) __attribute__((always_inline)) {
+        if (s >= steps) return;
+        p.template load<decltype(slot)::value>();
+        q.template load<decltype(slot)::value>();
+    };
+    auto step = [&](auto slot, int s) __attribute__((always_inline)) {
+        float *lp = lds[s & 1], *lq = lp + kBK * kPLd;
+        p.template stage<decltype(slot)::value>(lp);
+        q.template stage<decltype(slot)::value>(lq);
         __syncthreads();   // (the other pair of stages is written after the next one, which everybody reaches behind its reads)
-        if (s + 1 < steps) {
-            p.load((s + 1) * kBK);
-            q.load((s + 1) * kBK);
-        }
+        request(slot, s + kAhead);
+        if (fragments <= 0) return;
 #pragma unroll
         for (int c = 0; c < kBK; c += 4) {
-            float fp[kF], fq[kF];
+            float fp[kP], fq[kQ];
 #pragma unroll
-            for (int i = 0; i < kF; ++i) {
-                fp[i] = lp[c * (TILE + 16) + at + wf + i * 16];
-                fq[i] = lq[c * (TILE + 16) + at + wr + i * 16];
+            for (int i = 0; i < kP; ++i) fp[i] = lp[c * kPLd + at_p + i * 16];
+#pragma unroll
+            for (int j = 0; j < kQ; ++j) fq[j] = lq[c * kQLd + at_q + j * (16 * kDown)];
+#pragma unroll
+            for (int j = 0; j < kQ; ++j) {
+                if (j >= fragments) break;
+#pragma unroll
+                for (int i = 0; i < kP; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fp[i], fq[j], acc[i][j], 0, 0, 0);
             }
-#pragma unroll
-            for (int i = 0; i < kF; ++i)
-#pragma unroll
-                for (int j = 0; j < kF; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fp[i], fq[j], acc[i][j], 0, 0, 0);
         }
+    };
+    using std::integral_constant;
+    request(integral_constant<int, 0>{}, begin);
+    request(integral_constant<int, 1>{}, begin + 1);
+    request(integral_constant<int, 2>{}, begin + 2);
+    request(integral_constant<int, 3>{}, begin + 3);
+    for (int s = begin; s < steps; s += kAhead) {
+        step(integral_constant<int, 0>{}, s);
+        if (s + 1 < steps) step(integral_constant<int, 1>{}, s + 1);
+        if (s + 2 < steps) step(integral_constant<int, 2>{}, s + 2);
+        if (s + 3 < steps) step(integral_constant<int, 3>{}, s + 3);
     }
+    float* out = static_cast<float*>(a.out) + out_at;
+    if (parts > 1) out = scratch + blockIdx.y * output_size(FORM, a) + out_at;
 #pragma unroll
-    for (int j = 0; j < kF; ++j) {
-        const int row = wr + j * 16 + lane % 16;
+    for (int j = 0; j < kQ; ++j) {
+        const int row = (wr + j * kDown) * 16 + lane % 16;
         if (row >= rows) continue;
 #pragma unroll
-        for (int i = 0; i < kF; ++i) {
+        for (int i = 0; i < kP; ++i) {
             const int f = wf + i * 16 + lane / 16 * 4;
-            if (f >= p.limit) continue;
-            O* to = out + (size_t)row * features + f;
+            float* to = out + (size_t)row * features + f;
             f32x4 v = acc[i][j];
-            if constexpr (FORM == kWgrad && sizeof(O) == 4)
-                if (a.accumulate) v += load4(to);
+            if constexpr (FORM == kWgrad)
+                if (parts == 1 && a.accumulate) v += load4(to);
             store4(to, v);
         }
     }
 }
 
-template <typename T, typename O, int FORM, int TILE>
-hipError_t launch(const Args& a, hipStream_t stream) {
-    const long f_tiles = ((FORM == kForward ? a.n : a.k) + TILE - 1) / TILE;
-    const long m_tiles = FORM == kWgrad ? (long)a.experts * ((a.n + TILE - 1) / TILE) : most_row_tiles(a.rows, a.experts, TILE);
-    product_kernel<T, O, FORM, TILE><<<dim3((unsigned)(f_tiles * m_tiles)), dim3(kThreads), 0, stream>>>(a);
-    return hipGetLastError();
+// Adds the parts of everything that the experts have.
+template <int FORM>
+__global__ __launch_bounds__(kThreads) void join_parts_kernel(Args a, int parts, const float* __restrict__ scratch) {
+    const int lane = threadIdx.x & 63;
+    int first, end;
+    expert_rows(a, lane, first, end);
+    const size_t size = output_size(FORM, a), at = ((size_t)blockIdx.x * kThreads + threadIdx.x) * 4;
+    if (FORM == kWgrad) {
+        if (at >= size) return;
+        const int e = (int)(at / ((size_t)a.n * a.k));   // (the same in the whole wavefront: a matrix is a multiple of 4096 numbers)
+        if (a.accumulate && __builtin_amdgcn_readlane(end - first, __builtin_amdgcn_readfirstlane(e)) == 0) return;
+    } else {
+        const size_t features = FORM == kForward ? a.n : a.k;
+        // rows from the first expert's first to the last one's end
+        const size_t row = at / features;
+        if (row < (size_t)__builtin_amdgcn_readlane(first, 0) || row >= (size_t)__builtin_amdgcn_readlane(end, a.experts - 1)) return;
+    }
+    f32x4 v = load4(scratch + at);
+    for (int s = 1; s < parts; ++s) v += load4(scratch + s * size + at);
+    float* to = static_cast<float*>(a.out) + at;
+    if (FORM == kWgrad && a.accumulate) v += load4(to);
+    store4(to, v);
 }
 
-template <typename T, typename O>
-hipError_t launch_form(Form form, const Args& a, hipStream_t stream) {
-    switch (form) {
-        case kForward: return launch<T, O, kForward, 64>(a, stream);
-        case kDgrad: return launch<T, O, kDgrad, 64>(a, stream);
-        default: return launch<T, O, kWgrad, 64>(a, stream);
-    }
+template <int FORM, int HEIGHT>
+hipError_t launch(const Args& a, float* scratch, hipStream_t stream) {
+    const long f_tiles = (FORM == kForward ? a.n : a.k) / kTileF;
+    const long m_tiles = FORM == kWgrad ? (long)a.experts * (a.n / HEIGHT) : most_row_tiles(a.rows, a.experts, HEIGHT);
+    const long tiles = f_tiles * m_tiles;
+    // Eight workgroups a CU, and 16 K steps each: with fewer the second kernel takes as long as what it saves.
+    const int depth = FORM == kForward ? a.k : FORM == kDgrad ? a.n : (a.rows + a.experts - 1) / a.experts;
+    long parts = kMostWorkgroups / tiles;
+    if (parts > depth / (16 * kBK)) parts = depth / (16 * kBK);
+    if (parts > (long)(kScratchFloats / output_size(FORM, a))) parts = (long)(kScratchFloats / output_size(FORM, a));
+    if (parts < 1) parts = 1;
+    product_kernel<FORM, HEIGHT><<<dim3((unsigned)tiles, (unsigned)parts), dim3(kThreads), 0, stream>>>(a, (int)parts, scratch);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess || parts == 1) return err;
+    const size_t size = output_size(FORM, a);
+    join_parts_kernel<FORM><<<dim3((unsigned)((size / 4 + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream>>>(a, (int)parts, scratch);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_f32(Form form, const Args& a, hipStream_t stream) { return launch_form<float, float>(form, a, stream); }
+hipError_t launch_f32(Form form, const Args& a, void* workspace, hipStream_t stream) {
+    float* scratch = static_cast<float*>(workspace);
+    const bool low = a.rows <= 16 * a.experts;   // 64 rows, 8 experts of 4096 x 4096: 209 us in tiles of 64, 141 in tiles of 16
+    switch (form) {
+        case kForward: return low ? launch<kForward, 16>(a, scratch, stream) : launch<kForward, 64>(a, scratch, stream);
+        case kDgrad: return low ? launch<kDgrad, 16>(a, scratch, stream) : launch<kDgrad, 64>(a, scratch, stream);
+        default: return launch<kWgrad, 64>(a, scratch, stream);
+    }
+}
 
 }  // namespace products
 }  // namespace moe

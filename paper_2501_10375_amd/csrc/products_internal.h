@@ -68,7 +68,8 @@ inline int persistent_grid() {
 }
 
 // Each enqueues a whole product and returns hipGetLastError().  `workspace`: product_workspace_bytes() of scratch.
-hipError_t launch_f32(Form form, const Args& a, hipStream_t stream);
+constexpr size_t kScratchFloats = (size_t)8 << 20;   // parts of fp32 products
+hipError_t launch_f32(Form form, const Args& a, void* workspace, hipStream_t stream);
 hipError_t launch_bf16(Form form, const Args& a, bool out_f32, void* workspace, hipStream_t stream);
 hipError_t launch_fp8(const Args& a, void* workspace, hipStream_t stream);
 // Forward products of few rows, of bf16 or (with scales) e4m3 matrices, and which calls have few.
