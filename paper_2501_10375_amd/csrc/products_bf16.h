@@ -94,7 +94,7 @@ struct TileKernel {
 
     // decode(n, Item&): this workgroup's n-th item, false if it has fewer.
     template <class Decode>
-    static __device__ GG_INLINE void run(const Args& a, float* scratch, int piece_units, unsigned char* lds, Item cur, const Decode& decode) {
+    static __device__ GG_INLINE void run(const Args& a, float* scratch, Told* told, int piece_units, unsigned char* lds, Item cur, const Decode& decode) {
         const int N = a.n, K = a.k;
         const int features = FORM == kForward ? N : K;
         const lds_ptr lds3 = (lds_ptr)lds;
@@ -303,6 +303,7 @@ struct TileKernel {
                 // [16 rows][128 features] fp32, rows of 512 bytes, 16-byte unit u of row r at u ^ r
                 const int unit = lane & 31, col = wq * 128 + unit * 4;
                 const bool piece = cur.piece >= 0;
+                tell_cut(told, cur, ((int64_t)(FORM == kWgrad ? cur.expert * (int64_t)N : 0) + cur.row0) * features + cur.f0, features);
                 const uint32_t stride = (uint32_t)(piece ? kTile : features) * 4u;
                 float* const tile_out = piece ? scratch + (size_t)cur.piece * piece_units * kUnitFloats
                                               : static_cast<float*>(a.out) + (size_t)cur.expert * N * K + (size_t)cur.row0 * features + cur.f0;
@@ -378,7 +379,7 @@ struct TileKernel {
 };
 
 template <int FORM, bool OUT32>
-__global__ __launch_bounds__(256, 1) void product_gemm_kernel(Args a, float* scratch, Plan* told) {
+__global__ __launch_bounds__(256, 1) void product_gemm_kernel(Args a, float* scratch, Told* told) {
     using Kernel = TileKernel<FORM, OUT32>;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[Kernel::kLdsBytes];
     Tiles<FORM, kStepC> list(a);
@@ -390,12 +391,12 @@ __global__ __launch_bounds__(256, 1) void product_gemm_kernel(Args a, float* scr
         plan = choose_tiles(list, FORM == kForward ? a.n : a.k, gridDim.x, {kTile, 90, 6});
         list.build(plan.height);
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0) *told = plan;
     const Items<FORM, kStepC> items(list, plan);
+    if (blockIdx.x == 0 && threadIdx.x == 0) told->plan = items.plan;
     const Hand<FORM, kStepC> hand(list, items);
     Item item;
     if (!hand(0, item)) return;
-    Kernel::run(a, scratch, plan.piece_units, lds, item, hand);
+    Kernel::run(a, scratch, told, plan.piece_units, lds, item, hand);
 }
 
 }  // namespace products

@@ -8,12 +8,12 @@ namespace {
 template <int FORM, bool OUT32>
 hipError_t launch(const Args& a, void* workspace, hipStream_t stream) {
     float* scratch = static_cast<float*>(workspace);
-    Plan* plan = reinterpret_cast<Plan*>(static_cast<char*>(workspace) + kScratchBytes);
+    Told* told = reinterpret_cast<Told*>(static_cast<char*>(workspace) + kScratchBytes);
     const int grid = persistent_grid();
-    product_gemm_kernel<FORM, OUT32><<<grid, 256, 0, stream>>>(a, scratch, plan);
+    product_gemm_kernel<FORM, OUT32><<<grid, 256, 0, stream>>>(a, scratch, told);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    join_pieces_kernel<FORM, kStepC, OUT32><<<kMostCutTiles * 8, 256, 0, stream>>>(a, scratch, plan);
+    join_pieces_kernel<OUT32><<<kJoinWorkgroups, 256, 0, stream>>>(a.out, FORM == kForward ? a.n : a.k, a.accumulate, scratch, told);
     return hipGetLastError();
 }
 
@@ -27,7 +27,7 @@ hipError_t launch_bf16(Form form, const Args& a, bool out_f32, void* workspace, 
     }
 }
 
-size_t product_workspace_bytes(const moe_product_t& p, int) { return p.dtype == MOE_F32 ? kScratchFloats * sizeof(float) : kScratchBytes + 256; }
+size_t product_workspace_bytes(const moe_product_t& p, int) { return p.dtype == MOE_F32 ? kScratchFloats * sizeof(float) : kWorkspaceBytes; }
 
 }  // namespace products
 }  // namespace moe

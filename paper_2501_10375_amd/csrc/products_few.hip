@@ -1,6 +1,6 @@
 // Grouped forward products of few rows: a stream over the weights of the experts that have any, bf16 or block-scaled e4m3.
 //
-// Bound by memory: a pass over an expert's weights serves 16 of its rows.  A workgroup takes 16 * FG features of an expert, its
+// Bound by memory: a pass over an expert's weights serves 16 * RF of its rows.  A workgroup takes 16 * FG features of an expert, its
 // wavefronts a share of the contraction each, and the weights go from memory straight to the registers that the matrix
 // instructions read: a load covers 16 features x 64 bytes, the next one the other halves of the same lines.  The rows come from the
 // caches the same way.  The wavefronts' sums meet in LDS.  (Loads that bypass the caches' replacement are slower: 16 rows through 8
@@ -18,14 +18,14 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 
 constexpr int kLine = 128;   // bytes of a K step
-constexpr int kRows = 16;
+constexpr int kRows = 16;    // of a fragment
 
 __device__ inline i32x4 load16(const char* p) { return *reinterpret_cast<const i32x4*>(p); }
 
-template <bool FP8, int FG, int WAVES>
+template <bool FP8, int RF, int FG, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void product_few_rows_kernel(Args a) {
-    constexpr int kFeatures = 16 * FG, kThreads = 64 * WAVES;
-    __shared__ float sums[WAVES][kRows][kFeatures + 1];
+    constexpr int kFeatures = 16 * FG, kThreads = 64 * WAVES, kPass = RF * kRows;
+    __shared__ float sums[WAVES][kPass][kFeatures + 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int f_tiles = a.n / kFeatures;
     const int nth = blockIdx.x / f_tiles, f0 = (blockIdx.x - nth * f_tiles) * kFeatures;
@@ -44,38 +44,50 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_rows_kernel(Args a) {
     const char* w = static_cast<const char*>(a.p) + ((size_t)e * a.n + f0 + lane % 16) * row_bytes + lane / 16 * 16;
     const float* w_scale = FP8 ? a.p_scales + ((size_t)e * nb + f0 / 128) * kb : nullptr;
 
-    for (int row0 = __builtin_amdgcn_readlane(first, e); row0 < row_end; row0 += kRows) {
-        const int rows = min(kRows, row_end - row0);
-        const size_t row = row0 + min(lane % 16, rows - 1);   // (rows past the end repeat the last one)
-        const char* x = static_cast<const char*>(a.q) + row * row_bytes + lane / 16 * 16;
-        const float* x_scale = FP8 ? a.q_scales + row * kb : nullptr;
-        f32x4 acc[FG];
+    for (int row0 = __builtin_amdgcn_readlane(first, e); row0 < row_end; row0 += kPass) {
+        const int rows = min(kPass, row_end - row0);
+        const char* x[RF];
+        const float* x_scale[RF];
+        f32x4 acc[RF][FG];
 #pragma unroll
-        for (int f = 0; f < FG; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int r = 0; r < RF; ++r) {
+            const size_t row = row0 + min(r * kRows + lane % 16, rows - 1);   // (rows past the end repeat the last one)
+            x[r] = static_cast<const char*>(a.q) + row * row_bytes + lane / 16 * 16;
+            x_scale[r] = FP8 ? a.q_scales + row * kb : nullptr;
+#pragma unroll
+            for (int f = 0; f < FG; ++f) acc[r][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
         auto step = [&](int s, bool second_half) __attribute__((always_inline)) {
             const size_t at = (size_t)s * kLine;
-            i32x4 wl[FG], wh[FG];
+            i32x4 wl[FG], wh[FG], xl[RF], xh[RF];
 #pragma unroll
             for (int f = 0; f < FG; ++f) {
                 wl[f] = load16(w + f * 16 * row_bytes + at);
                 wh[f] = second_half ? load16(w + f * 16 * row_bytes + at + 64) : i32x4{0, 0, 0, 0};
             }
-            const i32x4 xl = load16(x + at), xh = second_half ? load16(x + at + 64) : i32x4{0, 0, 0, 0};
-            if constexpr (FP8) {
-                const float by = x_scale[s] * w_scale[s];
-                const i32x8 q = __builtin_shufflevector(xl, xh, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-                for (int f = 0; f < FG; ++f) {
-                    const i32x8 p = __builtin_shufflevector(wl[f], wh[f], 0, 1, 2, 3, 4, 5, 6, 7);
-                    const f32x4 d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+            for (int r = 0; r < RF; ++r) {
+                xl[r] = load16(x[r] + at);
+                xh[r] = second_half ? load16(x[r] + at + 64) : i32x4{0, 0, 0, 0};
+            }
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) acc[f][c] = fmaf(d[c], by, acc[f][c]);
-                }
-            } else {
+            for (int r = 0; r < RF; ++r) {
+                if constexpr (FP8) {
+                    const float by = x_scale[r][s] * w_scale[s];
+                    const i32x8 q = __builtin_shufflevector(xl[r], xh[r], 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-                for (int f = 0; f < FG; ++f) {
-                    acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wl[f]), __builtin_bit_cast(bf16x8, xl), acc[f], 0, 0, 0);
-                    acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wh[f]), __builtin_bit_cast(bf16x8, xh), acc[f], 0, 0, 0);
+                    for (int f = 0; f < FG; ++f) {
+                        const i32x8 p = __builtin_shufflevector(wl[f], wh[f], 0, 1, 2, 3, 4, 5, 6, 7);
+                        const f32x4 d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) acc[r][f][c] = fmaf(d[c], by, acc[r][f][c]);
+                    }
+                } else {
+#pragma unroll
+                    for (int f = 0; f < FG; ++f) {
+                        acc[r][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wl[f]), __builtin_bit_cast(bf16x8, xl[r]), acc[r][f], 0, 0, 0);
+                        acc[r][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wh[f]), __builtin_bit_cast(bf16x8, xh[r]), acc[r][f], 0, 0, 0);
+                    }
                 }
             }
         };
@@ -89,11 +101,13 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_rows_kernel(Args a) {
         for (; s < whole; ++s) step(s, true);
         if (ragged && s < stop) step(s, false);
 
-        // A result: lane l holds row l % 16 and features 4 * (l / 16) + 0 .. 3 of its fragment.
+        // A result: lane l holds row l % 16 and features 4 * (l / 16) + 0 .. 3 of its fragments.
 #pragma unroll
-        for (int f = 0; f < FG; ++f)
+        for (int r = 0; r < RF; ++r)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) sums[wave][lane % 16][f * 16 + lane / 16 * 4 + c] = acc[f][c];
+            for (int f = 0; f < FG; ++f)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) sums[wave][r * kRows + lane % 16][f * 16 + lane / 16 * 4 + c] = acc[r][f][c];
         __syncthreads();
         for (int i = threadIdx.x; i < rows * (kFeatures / 2); i += kThreads) {
             const int row = i / (kFeatures / 2), f = i % (kFeatures / 2) * 2;
@@ -109,28 +123,45 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_rows_kernel(Args a) {
     }
 }
 
-template <bool FP8, int FG, int WAVES>
+template <bool FP8, int RF, int FG, int WAVES>
 hipError_t launch(const Args& a, int active, hipStream_t stream) {
-    product_few_rows_kernel<FP8, FG, WAVES><<<dim3((unsigned)(active * (a.n / (16 * FG)))), 64 * WAVES, 0, stream>>>(a);
+    product_few_rows_kernel<FP8, RF, FG, WAVES><<<dim3((unsigned)(active * (a.n / (16 * FG)))), 64 * WAVES, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-// Up to 16 rows a pass over the weights of every expert that has any is all that is needed; beyond, as long as the experts have few on average, see the
-// times of this kernel / of the tile kernels in us (experts, out, in features, rows): bf16 8, 14336, 4096, 16 154 / 181, 32 171 / 186, 64 188 / 191, 128 259 / 198;
-// 8, 4096, 14336, 32 192 / 187, 64 195 / 177; 64, 1408, 2048, 64 44 / 55, 240 68 / 92; 1, 6400, 4096, 16 17 / 22, 64 59 / 30; 8 bits 8, 14336, 4096, 16 80 / 102, 64
-// 84 / 106, 128 112 / 111; 16, 6400, 4096, 32 72 / 101; 64, 1408, 2048, 240 35 / 49; 1, 14336, 4096, 32 26 / 25.
-bool few_rows(const Args& a, bool fp8) { return a.rows <= kRows || a.rows <= (fp8 ? 8 : 4) * a.experts; }
+namespace {
+int most_active(const Args& a) { return a.experts < a.rows ? a.experts : a.rows; }   // experts with rows
+}  // namespace
 
-// Two feature fragments for 8 bits beyond 16 rows: the rows' loads and scales serve both (8, 14336, 4096, 64: 99 -> 84 us; bf16 188 -> 203).
+// Which calls: where the experts have few rows on average, and, as long as the weights are read fast (256 MiB are what the memory-side cache
+// holds), up to 24 or 32, because a call of the tile kernels has two launches and some 10 us that are not streaming.  Times of this kernel / of
+// the tile kernels in us (experts, out, in features, rows).  bf16: 8, 14336, 4096, 16 154 / 181, 32 171 / 186, 64 188 / 191, 128 259 / 198; 8, 4096, 14336, 32
+// 192 / 187, 64 195 / 177; 64, 1408, 2048, 64 44 / 55, 240 68 / 92, 300 69 / 85, 512 88 / 100; 8, 4096, 4096, 64 53 / 74, 100 66 / 78; 4, 4096, 4096, 100 43 / 39; 1, 4096, 4096, 32 18 / 33; 8, 1024, 2048, 200
+// 19 / 27.  8 bits: 8, 14336, 4096, 16 80 / 102, 64 84 / 109, 154 90 / 99, 200 104 / 102; 16, 6400, 4096, 32 72 / 101, 150 87 / 93, 300 91 / 88; 64, 1408, 2048, 512 41 / 48, 1024
+// 97 / 45; 4, 2048, 2048, 60 12 / 18; 16, 1024, 1024, 300 12 / 14.
+bool few_rows(const Args& a, bool fp8) {
+    const size_t bytes = (size_t)most_active(a) * a.n * a.k * (fp8 ? 1 : 2);
+    const bool cached = bytes <= (size_t)256 << 20, small = bytes <= (size_t)64 << 20;
+    return a.rows <= kRows || a.rows <= (fp8 ? 8 : 4) * a.experts || (fp8 && a.rows <= 160 && a.rows <= 20 * a.experts) ||
+           (cached && a.rows <= 320 && a.rows <= (small ? 32 : 24) * a.experts);
+}
+
+// One fragment of rows a pass up to eight rows an expert, two beyond; feature fragments that share the rows' loads where there are workgroups enough
+// (8 bits 8, 14336, 4096, 64 in ones, twos, fours: 101, 84, 83 us; 154 with two of rows: -, 106, 90; 1, 4096, 4096, 24: -, 11, 14; bf16 8, 14336, 4096, 64: 188, 203, 204).
 // Eight wavefronts where four would leave the CUs with few and each still has 16 K steps (bf16 8, 4096, 14336, 2: 42 -> 37 us; with less, 8 bits
 // 16, 6400, 4096, 2: 12.2 -> 15.4).
 hipError_t launch_few_rows(const Args& a, bool fp8, hipStream_t stream) {
-    const int active = a.experts < a.rows ? a.experts : a.rows;   // experts with rows, at most
-    const bool eight = (long)active * (a.n / 16) <= 4L * compute_units() && a.k / 64 >= 8 * 16;
-    if (!fp8) return eight ? launch<false, 1, 8>(a, active, stream) : launch<false, 1, 4>(a, active, stream);
-    return a.rows <= kRows ? launch<true, 1, 4>(a, active, stream) : launch<true, 2, 4>(a, active, stream);
+    const int active = most_active(a);
+    const bool one = a.rows <= kRows || a.rows <= 8 * a.experts;
+    if (!fp8) {
+        const bool eight = (long)active * (a.n / 16) <= 4L * compute_units() && a.k / 64 >= 8 * 16;
+        return !one ? launch<false, 2, 2, 4>(a, active, stream) : eight ? launch<false, 1, 1, 8>(a, active, stream) : launch<false, 1, 1, 4>(a, active, stream);
+    }
+    if (a.rows <= kRows) return launch<true, 1, 1, 4>(a, active, stream);
+    if (one) return launch<true, 1, 2, 4>(a, active, stream);
+    return (long)active * (a.n / 64) <= 2L * compute_units() ? launch<true, 2, 2, 4>(a, active, stream) : launch<true, 2, 4, 4>(a, active, stream);
 }
 
 }  // namespace products

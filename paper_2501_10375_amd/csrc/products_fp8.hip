@@ -71,7 +71,7 @@ struct Fp8Kernel {
     }
 
     template <class Decode>
-    static __device__ GG_INLINE void run(const Args& a, float* scratch, int piece_units, unsigned char* lds, Item cur, const Decode& decode) {
+    static __device__ GG_INLINE void run(const Args& a, float* scratch, Told* told, int piece_units, unsigned char* lds, Item cur, const Decode& decode) {
         const int N = a.n, K = a.k, kb = (K + 127) / 128, nb = (N + 127) / 128;
         const lds_ptr lds3 = (lds_ptr)lds;
         const uint32_t lds0 = (uint32_t)(uintptr_t)lds3;
@@ -312,6 +312,7 @@ struct Fp8Kernel {
             } else {
                 // [16 rows][64 features] fp32, rows of 256 bytes, 16-byte unit u of row r at u ^ r
                 const int col = wq * 64 + frow * 4;
+                tell_cut(told, cur, (int64_t)cur.row0 * N + cur.f0, N);
                 const __amdgpu_buffer_rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(scratch + (size_t)cur.piece * piece_units * kUnitFloats, 0,
                                                                                     cur.rows * kTile * 4, 0x00020000);
                 const uint32_t to = cur.f0 + col < N ? (uint32_t)((wt * 16 + fpiece) * kTile + col) * 4u : kNowhere;
@@ -346,28 +347,28 @@ struct Fp8Kernel {
     }
 };
 
-__global__ __launch_bounds__(Fp8Kernel::kThreads, 1) void product_fp8_kernel(Args a, float* scratch, Plan* told) {
+__global__ __launch_bounds__(Fp8Kernel::kThreads, 1) void product_fp8_kernel(Args a, float* scratch, Told* told) {
     __shared__ __attribute__((aligned(1024))) unsigned char lds[Fp8Kernel::kLdsBytes];
     Tiles<kForward, kStepC> list(a);
     const Plan plan = choose_tiles(list, a.n, gridDim.x, {kTallest, 60, 13});
     list.build(plan.height);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *told = plan;
     const Items<kForward, kStepC> items(list, plan);
+    if (blockIdx.x == 0 && threadIdx.x == 0) told->plan = items.plan;
     const Hand<kForward, kStepC> hand(list, items);
     Item item;
     if (!hand(0, item)) return;
-    Fp8Kernel::run(a, scratch, plan.piece_units, lds, item, hand);
+    Fp8Kernel::run(a, scratch, told, plan.piece_units, lds, item, hand);
 }
 
 }  // namespace
 
 hipError_t launch_fp8(const Args& a, void* workspace, hipStream_t stream) {
     float* scratch = static_cast<float*>(workspace);
-    Plan* plan = reinterpret_cast<Plan*>(static_cast<char*>(workspace) + kScratchBytes);
-    product_fp8_kernel<<<persistent_grid(), Fp8Kernel::kThreads, 0, stream>>>(a, scratch, plan);
+    Told* told = reinterpret_cast<Told*>(static_cast<char*>(workspace) + kScratchBytes);
+    product_fp8_kernel<<<persistent_grid(), Fp8Kernel::kThreads, 0, stream>>>(a, scratch, told);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    join_pieces_kernel<kForward, kStepC, false><<<kMostCutTiles * 8, 256, 0, stream>>>(a, scratch, plan);
+    join_pieces_kernel<false><<<kJoinWorkgroups, 256, 0, stream>>>(a.out, a.n, 0, scratch, told);
     return hipGetLastError();
 }
 

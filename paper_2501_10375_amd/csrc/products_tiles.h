@@ -19,7 +19,7 @@ constexpr int kXcds = gg::kXcds;
 constexpr int kUnitRows = 32, kScratchUnits = 255 * 8;
 constexpr size_t kUnitFloats = (size_t)kUnitRows * kTile;
 constexpr size_t kScratchBytes = kScratchUnits * kUnitFloats * sizeof(float);
-constexpr int kMostCutTiles = 255;   // (the leftover tiles of a round of at most 256)
+constexpr int kMostCutTiles = 255;   // (the leftover tiles of a round of at most 256 workgroups)
 constexpr int kMinPartSteps = 3;   // fewest K steps of a piece
 
 // What a launch does, the same in every wavefront: chosen when its kernel starts and left in the workspace for the one that
@@ -30,7 +30,21 @@ struct Plan {
     int parts;         // forward, dgrad: pieces of the others
     int chunk;         // wgrad: K steps of a piece
     int piece_units;   // units of scratch of a piece
+    int n_cuts;        // tiles that are cut
 };
+
+// A tile that was cut, for the kernel that joins its pieces.
+struct Cut {
+    int64_t out_at;         // element of the output of its first row and feature
+    int rows, columns;      // that exist
+    int first_piece, parts;
+};
+// What a launch leaves behind its pieces.
+struct Told {
+    Plan plan;
+    Cut cuts[kMostCutTiles];
+};
+constexpr size_t kWorkspaceBytes = (kScratchBytes + sizeof(Told) + 255) / 256 * 256;
 
 // The tiles of a launch, expert by expert in descending order of rows; lane r holds the expert of rank r.  Within an expert
 // row tiles in groups of at most eight of nearly equal size, within a group feature tile by feature tile: 32 consecutive tiles are
@@ -101,24 +115,25 @@ struct Price {
 };
 
 // Height of the tiles and pieces of the leftover ones (forward, dgrad), like choose_plan() of the expert GEMMs: lane l prices one
-// of 30 plans (the tallest tile - 32 * (l / 6) rows, l % 6 + 1 pieces) in 10 ns, as the larger of
+// of 60 plans (the tallest tile - 32 * (l / 12) rows; 1 to 6, 8, 10, 12, 16, 20 or 24 pieces) in 10 ns, as the larger of
 //   full rounds x (K steps x their price + 400) and the same for the rounds of pieces                  (MFMAs)
 //   the weights of the experts with rows at 6.6 TB/s + 600 a round                                   (memory)
 // + 300 + 2 a unit of pieces, if there are any; the first of the cheapest is taken.
 template <class List>
 __device__ GG_INLINE Plan choose_tiles(const List& list, int features, int grid, Price price) {
     const int lane = threadIdx.x & 63;
-    const int i = min(lane / 6, 4), p = lane - lane / 6 * 6 + 1, h = price.tallest - 32 * i;
+    const int i = min(lane / 12, 4), n = lane - lane / 12 * 12, h = price.tallest - 32 * i;
+    const int p = n < 6 ? n + 1 : n < 9 ? 2 * n - 4 : 4 * n - 20;
     int sums[5];
 #pragma unroll
-    for (int n = 0; n < 5; ++n) sums[n] = list.row_tiles(price.tallest - 32 * n);
+    for (int t = 0; t < 5; ++t) sums[t] = list.row_tiles(price.tallest - 32 * t);
     const int most = __builtin_amdgcn_readlane(list.count, 0);
     const int active = __popcll(__ballot(list.count > 0));
     const int steps = __builtin_amdgcn_readlane(list.steps(), 0);
     gg::wave_totals(sums);
     int tiles = sums[0];
 #pragma unroll
-    for (int n = 1; n < 5; ++n) tiles = i == n ? sums[n] : tiles;
+    for (int t = 1; t < 5; ++t) tiles = i == t ? sums[t] : tiles;
     tiles *= list.n_ft;
     const int full = tiles / grid, left = tiles - full * grid;
     const int units = (min(h, most) + kUnitRows - 1) / kUnitRows;
@@ -128,7 +143,7 @@ __device__ GG_INLINE Plan choose_tiles(const List& list, int features, int grid,
     const float work = full * (steps * step + 400.f) + rounds * ((steps + p - 1) / p * step + 400.f);
     const float stream = active * (float)features * steps * (1.f / 516.f) + (full + rounds) * 600.f;
     float cost = fmaxf(work, stream) + (p > 1 ? 300.f + 2.f * left * units * p : 0.f);
-    if (lane >= 30 || !allowed) cost = INFINITY;
+    if (lane >= 60 || !allowed) cost = INFINITY;
     float best = cost;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) best = fminf(best, __shfl_xor(best, d, 64));
@@ -181,27 +196,34 @@ struct Items {
     const Tiles<FORM, STEP>& list;
     Plan plan;
     int total, left;
-    int first_item, parts, first_piece;   // wgrad, lane r
+    int first_item, parts, first_piece, first_cut;   // wgrad, lane r
 
     __device__ GG_INLINE Items(const Tiles<FORM, STEP>& l, const Plan& p) : list(l), plan(p) {
-        first_item = parts = first_piece = 0;
+        first_item = parts = first_piece = first_cut = 0;
         if constexpr (FORM == kWgrad) {
             const int tiles = list.row_tiles(list.height) * list.n_ft;
             parts = list.parts_of(plan.chunk);
-            const int sum = gg::wave_inclusive_sum(tiles * parts), cut = gg::wave_inclusive_sum(parts > 1 ? tiles * parts : 0);
+            const int cut = parts > 1 ? tiles : 0;
+            const int sum = gg::wave_inclusive_sum(tiles * parts), pieces = gg::wave_inclusive_sum(cut * parts), cuts = gg::wave_inclusive_sum(cut);
             first_item = sum - tiles * parts;
-            first_piece = cut - (parts > 1 ? tiles * parts : 0);
+            first_piece = pieces - cut * parts;
+            first_cut = cuts - cut;
             total = __builtin_amdgcn_readlane(sum, 63);
             left = 0;
+            plan.n_cuts = __builtin_amdgcn_readlane(cuts, 63);
         } else {
             left = list.total - plan.n_whole;
             total = plan.n_whole + left * plan.parts;
+            plan.n_cuts = plan.parts > 1 ? left : 0;
         }
     }
-    // Item `id`: its tile, the K steps [begin, end) of it, and the number of its piece (-1: it is a whole tile).
-    __device__ GG_INLINE void find(int id, int& tile, int& begin, int& end, int& piece) const {
-        int part = 0, of = 1, steps;
-        piece = -1;
+    // Item `id`: its tile, the K steps [begin, end) of it, the number of its piece (-1: it is a whole tile), which part of how many that is, and the number of
+    // its tile among those that are cut.
+    __device__ GG_INLINE void find(int id, int& tile, int& begin, int& end, int& piece, int& part, int& of, int& cut) const {
+        int steps;
+        part = 0;
+        of = 1;
+        piece = cut = -1;
         if constexpr (FORM == kWgrad) {
             const int r = __popcll(__ballot(first_item <= id && list.count > 0)) - 1;
             of = __builtin_amdgcn_readlane(parts, r);
@@ -210,16 +232,19 @@ struct Items {
             part = local / tiles;
             tile = first + local - part * tiles;
             steps = __builtin_amdgcn_readlane(list.steps(), r);
-            if (of > 1) piece = __builtin_amdgcn_readlane(first_piece, r) + (tile - first) * of + part;
+            if (of > 1) {
+                cut = __builtin_amdgcn_readlane(first_cut, r) + tile - first;
+                piece = __builtin_amdgcn_readlane(first_piece, r) + (tile - first) * of + part;
+            }
         } else {
             tile = id;
             steps = __builtin_amdgcn_readlane(list.steps(), 0);
             if (id >= plan.n_whole && plan.parts > 1) {
                 of = plan.parts;
                 part = (id - plan.n_whole) / left;
-                const int t = id - plan.n_whole - part * left;
-                tile = plan.n_whole + t;
-                piece = t * of + part;
+                cut = id - plan.n_whole - part * left;
+                tile = plan.n_whole + cut;
+                piece = cut * of + part;
             }
         }
         begin = steps * part / of;
@@ -232,6 +257,7 @@ struct Item {
     int expert, row0, rows, f0, k_steps, depth;   // row0: first output row (forward, dgrad: of the matrix; wgrad: of the expert's)
     int c0;                                       // first c: wgrad: row of the matrix, else of the contraction; depth: c from there on
     int piece;                                    // number of the piece, -1: a whole tile
+    int cut, parts;                               // first piece of a tile that is cut: which one that is (else -1), and its pieces
 };
 
 // A workgroup's items.  The launch is persistent, one workgroup a CU.  Workgroup b belongs to XCD b % 8 (the hardware deals them out
@@ -257,8 +283,10 @@ struct Hand {
             id = full * grid + xcd * share + member;
             if (id >= items.total) return false;
         }
-        int tile, begin, end, r, row, ft;
-        items.find(id, tile, begin, end, t.piece);
+        int tile, begin, end, r, row, ft, part;
+        items.find(id, tile, begin, end, t.piece, part, t.parts, t.cut);
+        t.cut = uniform(part == 0 ? t.cut : -1);
+        t.parts = uniform(t.parts);
         list.find(tile, r, row, t.rows, ft);
         t.expert = __builtin_amdgcn_readlane(list.rank_expert, r);
         const int first = __builtin_amdgcn_readlane(list.first, r);
@@ -328,52 +356,33 @@ struct Buffer {
     }
 };
 
-// Adds the pieces of the tiles that were cut: 32 rows of one of them for each workgroup.
-template <int FORM, int STEP, bool OUT32>
-__global__ __launch_bounds__(256) void join_pieces_kernel(Args a, const float* __restrict__ scratch, const Plan* told) {
-    const Plan plan = *told;
-    if (FORM != kWgrad && plan.parts <= 1) return;
-    const int cut = blockIdx.x / 8, unit = blockIdx.x % 8;   // number of the cut tile, and which rows of it
-    Tiles<FORM, STEP> list(a);
-    list.build(plan.height);
-    const Items<FORM, STEP> items(list, plan);
-    int tile, r, row, rows, ft, parts, piece;
-    if constexpr (FORM == kWgrad) {
-        const int cut_tiles = items.parts > 1 ? list.row_tiles(list.height) * list.n_ft : 0;
-        const int sum = gg::wave_inclusive_sum(cut_tiles);
-        if (cut >= __builtin_amdgcn_readlane(sum, 63)) return;
-        const int owner = __popcll(__ballot(sum <= cut));   // (experts that are cut come first: they have most rows)
-        const int local = cut - __builtin_amdgcn_readlane(sum - cut_tiles, owner);
-        tile = __builtin_amdgcn_readlane(list.first_tile, owner) + local;
-        parts = __builtin_amdgcn_readlane(items.parts, owner);
-        piece = __builtin_amdgcn_readlane(items.first_piece, owner) + local * parts;
-    } else {
-        if (cut >= items.left) return;
-        tile = plan.n_whole + cut;
-        parts = plan.parts;
-        piece = cut * parts;
-    }
-    list.find(tile, r, row, rows, ft);
-    const int features = FORM == kForward ? a.n : a.k;
-    const int expert = __builtin_amdgcn_readlane(list.rank_expert, r);
-    const int64_t row0 = (FORM == kWgrad ? (int64_t)expert * a.n : (int64_t)__builtin_amdgcn_readlane(list.first, r)) + row;
-    const int col = threadIdx.x % 64 * 4, f = ft * kTile + col;
-    if (f >= features) return;
-    const size_t piece_floats = (size_t)plan.piece_units * kUnitFloats;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int at = unit * kUnitRows + i * 4 + threadIdx.x / 64;
-        if (at >= rows) break;
-        const float* from = scratch + (size_t)piece * piece_floats + (size_t)at * kTile + col;
+// The first piece of a tile tells the kernel that joins them where it belongs (out_at: element of its first row and feature).
+__device__ GG_INLINE void tell_cut(Told* told, const Item& t, int64_t out_at, int features) {
+    if (t.cut >= 0 && threadIdx.x == 0) told->cuts[t.cut] = Cut{out_at, t.rows, min(kTile, features - t.f0), t.piece, t.parts};
+}
+
+// Adds the pieces of the tiles that were cut: four rows of one of them at a time for each workgroup, a thread four columns of a row.
+constexpr int kJoinWorkgroups = 1024;
+template <bool OUT32>
+__global__ __launch_bounds__(256) void join_pieces_kernel(void* out, int features, int accumulate, const float* __restrict__ scratch, const Told* __restrict__ told) {
+    const int units = told->plan.piece_units, groups = units * (kUnitRows / 4), total = told->plan.n_cuts * groups;
+    const size_t piece_floats = (size_t)units * kUnitFloats;
+    const int col = threadIdx.x % 64 * 4;
+    for (int g = blockIdx.x; g < total; g += kJoinWorkgroups) {
+        const Cut cut = told->cuts[g / groups];
+        const int row = g % groups * 4 + threadIdx.x / 64;
+        if (row >= cut.rows || col >= cut.columns) continue;
+        const float* from = scratch + (size_t)cut.first_piece * piece_floats + (size_t)row * kTile + col;
         f32x4 v = *reinterpret_cast<const f32x4*>(from);
-        for (int s = 1; s < parts; ++s) v += *reinterpret_cast<const f32x4*>(from + s * piece_floats);
-        const size_t to = (size_t)(row0 + at) * features + f;
+#pragma unroll 8
+        for (int s = 1; s < cut.parts; ++s) v += *reinterpret_cast<const f32x4*>(from + s * piece_floats);
+        const size_t to = (size_t)cut.out_at + (size_t)row * features + col;
         if constexpr (OUT32) {
-            f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to);
-            if (a.accumulate) v += *o;
+            f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(out) + to);
+            if (accumulate) v += *o;
             *o = v;
         } else {
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + to) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + to) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
         }
     }
 }
