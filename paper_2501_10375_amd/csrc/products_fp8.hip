@@ -150,7 +150,7 @@ struct Fp8Kernel {
         const int frow = lane & 15, fpiece = lane >> 4;
         const uint32_t in_row = (uint32_t)(frow * 128 + ((((frow >> 1) & 7) ^ fpiece) << 4));
         const uint32_t p_read = (uint32_t)(wq * 64) * 128 + in_row, q_read = kQBase + (uint32_t)wt * 2048 + in_row;
-        const uint32_t x_read = kSBase + (uint32_t)(wt * 16 + frow) * 16, w_read = kSBase + 3072 + (uint32_t)(wq >> 1) * 16;
+        const uint32_t x_read = kSBase + (uint32_t)(wt * 16 + frow) * 16, w_read = kSBase + 3 * 1024 + (uint32_t)(wq >> 1) * 16;
         auto fragment = [&](uint32_t at, int rows) GG_LAMBDA {
             typedef __attribute__((address_space(3))) const i32x4* piece;
             const i32x4 lo = *reinterpret_cast<piece>(lds3 + at + rows * 128), hi = *reinterpret_cast<piece>(lds3 + (at ^ 64u) + rows * 128);

@@ -141,4 +141,4 @@ def test_binding_refuses_cpu_tensors_and_other_types():
     with pytest.raises(ValueError):
         products.moe_quantize_rows_fp8(x, y.to(torch.uint8), torch.zeros(4, 1))
     with pytest.raises(TypeError):   # the numbers have to be e4m3
-        products._e4m3(y, (4, 64), "q")
+        products._e4m3(y, (4, 64), "q", 0)
