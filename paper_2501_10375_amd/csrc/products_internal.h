@@ -26,6 +26,20 @@ struct Args {
     int accumulate;                   // kWgrad
 };
 
+// Inclusive sums over a wavefront by DPP: shifts within rows of 16 lanes, then the last lane of a row (of two rows) to the next one.  (Some ten
+// cycles a step; by __shfl_up, which goes through LDS, more than a hundred, all of them ahead of a launch's first load.)
+template <int CTRL, int ROWS>
+__device__ inline int lanes_before(int other, int v) { return __builtin_amdgcn_update_dpp(other, v, CTRL, ROWS, 0xf, false); }
+__device__ inline int wave_sums(int v) {
+    v += lanes_before<0x111, 0xf>(0, v);
+    v += lanes_before<0x112, 0xf>(0, v);
+    v += lanes_before<0x114, 0xf>(0, v);
+    v += lanes_before<0x118, 0xf>(0, v);
+    v += lanes_before<0x142, 0xa>(0, v);
+    v += lanes_before<0x143, 0xc>(0, v);
+    return v;
+}
+
 // First and one past the last row of lane `lane`'s expert, inside [0, rows] whatever the table holds.
 __device__ inline void expert_rows(const Args& a, int lane, int& first, int& end) {
     first = end = 0;
@@ -46,12 +60,7 @@ __device__ inline bool find_row_tile(const Args& a, int tile, int height, int& e
     int first, end;
     expert_rows(a, lane, first, end);
     const int tiles = (end - first + height - 1) / height;
-    int sum = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int u = __shfl_up(sum, d, 64);
-        if (lane >= d) sum += u;
-    }
+    const int sum = wave_sums(tiles);
     if (tile >= __builtin_amdgcn_readlane(sum, 63)) return false;
     expert = __popcll(__ballot(sum <= tile));
     const int m = tile - __builtin_amdgcn_readlane(sum - tiles, expert);

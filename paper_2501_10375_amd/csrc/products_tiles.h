@@ -46,6 +46,18 @@ struct Told {
 };
 constexpr size_t kWorkspaceBytes = (kScratchBytes + sizeof(Told) + 255) / 256 * 256;
 
+template <int CTRL, int ROWS>
+__device__ GG_INLINE float least_before(float v) { return fminf(v, __int_as_float(lanes_before<CTRL, ROWS>(0x7f800000, __float_as_int(v)))); }
+__device__ GG_INLINE float wave_min(float v) {   // like wave_sums()
+    v = least_before<0x111, 0xf>(v);
+    v = least_before<0x112, 0xf>(v);
+    v = least_before<0x114, 0xf>(v);
+    v = least_before<0x118, 0xf>(v);
+    v = least_before<0x142, 0xa>(v);
+    v = least_before<0x143, 0xc>(v);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
 // The tiles of a launch, expert by expert in descending order of rows; lane r holds the expert of rank r.  Within an expert
 // row tiles in groups of at most eight of nearly equal size, within a group feature tile by feature tile: 32 consecutive tiles are
 // what the CUs of an XCD work on at a time, and share operand lines through its L2.
@@ -61,11 +73,13 @@ struct Tiles {
         int f, end;
         expert_rows(a, lane, f, end);
         const int rows = lane < a.experts ? end - f : -1;
-        int rank = lane < a.experts ? 0 : lane;
-        for (int i = 0; i < a.experts; ++i) {
-            const int ri = __builtin_amdgcn_readlane(rows, i);
-            if (lane < a.experts) rank += (ri > rows || (ri == rows && i < lane)) ? 1 : 0;
-        }
+        // Rows first, lower experts first among equals, lanes without an expert last.  (Four in a step: one has to wait for the other.)
+        const int key = lane < a.experts ? rows * 64 + 63 - lane : -lane;
+        int rank = 0;
+        for (int i = 0; i < a.experts; i += 4)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) rank += __builtin_amdgcn_readlane(key, i + j) > key ? 1 : 0;
+        rank = lane < a.experts ? rank : lane;
         rank_expert = __builtin_amdgcn_ds_permute(rank * 4, lane);
         first = __builtin_amdgcn_ds_permute(rank * 4, f);
         const int own = __builtin_amdgcn_ds_permute(rank * 4, rows);
@@ -75,7 +89,7 @@ struct Tiles {
         count = FORM != kWgrad ? own : own < 0 || (own == 0 && a.accumulate) ? 0 : a.n;
         height = total = first_tile = 0;
     }
-    __device__ GG_INLINE int row_tiles(int h) const { return count > 0 ? (count + h - 1) / h : 0; }
+    __device__ GG_INLINE int row_tiles(int h) const { return count > 0 ? (int)((uint32_t)(count + h - 1) / (uint32_t)h) : 0; }
     __device__ GG_INLINE int steps() const { return depth > 0 ? (depth + STEP - 1) / STEP : 1; }  // (no rows: one step of zeros)
 
     // wgrad: pieces of a tile of this lane's expert.
@@ -84,7 +98,7 @@ struct Tiles {
     __device__ GG_INLINE void build(int h) {
         height = h;
         const int tiles = row_tiles(h) * n_ft;
-        const int sum = gg::wave_inclusive_sum(tiles);
+        const int sum = wave_sums(tiles);
         first_tile = sum - tiles;
         total = __builtin_amdgcn_readlane(sum, 63);
     }
@@ -93,16 +107,16 @@ struct Tiles {
         r = __popcll(__ballot(first_tile <= id && count > 0)) - 1;
         const int c = __builtin_amdgcn_readlane(count, r);
         const int local = id - __builtin_amdgcn_readlane(first_tile, r);
-        const int mt = (c + height - 1) / height;
-        const int groups = (mt + kGroup - 1) / kGroup;
-        const int size = mt / groups, big = mt - size * groups;   // `big` groups of size + 1 row tiles, then groups of `size`
+        const uint32_t mt = (uint32_t)(c + height - 1) / (uint32_t)height;
+        const uint32_t groups = (mt + kGroup - 1) / kGroup;
+        const int size = (int)(mt / groups), big = mt - size * groups;   // `big` groups of size + 1 row tiles, then groups of `size`
         const int in_big = big * (size + 1) * n_ft;
         const bool b = local < in_big;
         const int gs = b ? size + 1 : size;
         const int in = b ? local : local - in_big;
-        const int g = in / (gs * n_ft);
+        const int g = (int)((uint32_t)in / (uint32_t)(gs * n_ft));
         const int in_grp = in - g * (gs * n_ft);
-        ft = in_grp / gs;
+        ft = (int)((uint32_t)in_grp / (uint32_t)gs);
         const int m = (b ? 0 : big * (size + 1)) + g * gs + in_grp - ft * gs;
         row = m * height;
         rows = min(height, c - row);
@@ -126,27 +140,24 @@ __device__ GG_INLINE Plan choose_tiles(const List& list, int features, int grid,
     const int p = n < 6 ? n + 1 : n < 9 ? 2 * n - 4 : 4 * n - 20;
     int sums[5];
 #pragma unroll
-    for (int t = 0; t < 5; ++t) sums[t] = list.row_tiles(price.tallest - 32 * t);
+    for (int t = 0; t < 5; ++t) sums[t] = __builtin_amdgcn_readlane(wave_sums(list.row_tiles(price.tallest - 32 * t)), 63);
     const int most = __builtin_amdgcn_readlane(list.count, 0);
     const int active = __popcll(__ballot(list.count > 0));
     const int steps = __builtin_amdgcn_readlane(list.steps(), 0);
-    gg::wave_totals(sums);
     int tiles = sums[0];
 #pragma unroll
     for (int t = 1; t < 5; ++t) tiles = i == t ? sums[t] : tiles;
     tiles *= list.n_ft;
-    const int full = tiles / grid, left = tiles - full * grid;
+    const int full = (int)((uint32_t)tiles / (uint32_t)grid), left = tiles - full * grid;
     const int units = (min(h, most) + kUnitRows - 1) / kUnitRows;
-    const int rounds = (left * p + grid - 1) / grid;
+    const int rounds = (int)((uint32_t)(left * p + grid - 1) / (uint32_t)grid);
     const bool allowed = p == 1 || (left > 0 && left * p * units <= kScratchUnits && steps >= p * kMinPartSteps);
     const float step = price.base + price.per_group * min(h, (most + 31) / 32 * 32) / 32;
-    const float work = full * (steps * step + 400.f) + rounds * ((steps + p - 1) / p * step + 400.f);
+    const float work = full * (steps * step + 400.f) + rounds * ((uint32_t)(steps + p - 1) / (uint32_t)p * step + 400.f);
     const float stream = active * (float)features * steps * (1.f / 516.f) + (full + rounds) * 600.f;
     float cost = fmaxf(work, stream) + (p > 1 ? 300.f + 2.f * left * units * p : 0.f);
     if (lane >= 60 || !allowed) cost = INFINITY;
-    float best = cost;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) best = fminf(best, __shfl_xor(best, d, 64));
+    const float best = wave_min(cost);
     const int winner = __ffsll((long long)__ballot(cost == best)) - 1;
     Plan plan;
     plan.height = __builtin_amdgcn_readlane(h, winner);
@@ -182,9 +193,7 @@ __device__ GG_INLINE Plan choose_chunk(const List& list, int grid, int n) {
     }
     float cost = (float)((pieces + grid - 1) / grid) * (chunk * 138.f + 400.f) + (cut > 0 ? 300.f + 2.f * cut * plan.piece_units : 0.f);
     if (cut * plan.piece_units > kScratchUnits) cost = INFINITY;
-    float best = cost;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) best = fminf(best, __shfl_xor(best, d, 64));
+    const float best = wave_min(cost);
     plan.chunk = __builtin_amdgcn_readlane(chunk, __ffsll((long long)__ballot(cost == best)) - 1);
     return plan;
 }
@@ -204,7 +213,7 @@ struct Items {
             const int tiles = list.row_tiles(list.height) * list.n_ft;
             parts = list.parts_of(plan.chunk);
             const int cut = parts > 1 ? tiles : 0;
-            const int sum = gg::wave_inclusive_sum(tiles * parts), pieces = gg::wave_inclusive_sum(cut * parts), cuts = gg::wave_inclusive_sum(cut);
+            const int sum = wave_sums(tiles * parts), pieces = wave_sums(cut * parts), cuts = wave_sums(cut);
             first_item = sum - tiles * parts;
             first_piece = pieces - cut * parts;
             first_cut = cuts - cut;
@@ -229,7 +238,7 @@ struct Items {
             of = __builtin_amdgcn_readlane(parts, r);
             const int first = __builtin_amdgcn_readlane(list.first_tile, r), local = id - __builtin_amdgcn_readlane(first_item, r);
             const int tiles = __builtin_amdgcn_readlane(list.row_tiles(list.height) * list.n_ft, r);
-            part = local / tiles;
+            part = (int)((uint32_t)local / (uint32_t)tiles);
             tile = first + local - part * tiles;
             steps = __builtin_amdgcn_readlane(list.steps(), r);
             if (of > 1) {
@@ -241,14 +250,14 @@ struct Items {
             steps = __builtin_amdgcn_readlane(list.steps(), 0);
             if (id >= plan.n_whole && plan.parts > 1) {
                 of = plan.parts;
-                part = (id - plan.n_whole) / left;
+                part = (int)((uint32_t)(id - plan.n_whole) / (uint32_t)left);
                 cut = id - plan.n_whole - part * left;
                 tile = plan.n_whole + cut;
                 piece = cut * of + part;
             }
         }
-        begin = steps * part / of;
-        end = steps * (part + 1) / of;
+        begin = of > 1 ? (int)((uint32_t)(steps * part) / (uint32_t)of) : 0;
+        end = of > 1 ? (int)((uint32_t)(steps * (part + 1)) / (uint32_t)of) : steps;
     }
 };
 
@@ -272,7 +281,7 @@ struct Hand {
         grid = gridDim.x;
         xcd = blockIdx.x % kXcds;
         member = blockIdx.x / kXcds;
-        full = items.total / grid;
+        full = (int)((uint32_t)items.total / (uint32_t)grid);
         share = (items.total - full * grid + kXcds - 1) / kXcds;
     }
     // This workgroup's n-th item; false if it has fewer.
