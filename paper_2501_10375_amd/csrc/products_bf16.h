@@ -388,7 +388,7 @@ __global__ __launch_bounds__(256, 1) void product_gemm_kernel(Args a, float* scr
         list.build(kTile);
         plan = choose_chunk(list, gridDim.x, a.n);
     } else {
-        plan = choose_tiles(list, FORM == kForward ? a.n : a.k, gridDim.x, {kTile, 90, 6});
+        plan = choose_tiles(list, gridDim.x, {kTile, 90, 6});
         list.build(plan.height);
     }
     const Items<FORM, kStepC> items(list, plan);

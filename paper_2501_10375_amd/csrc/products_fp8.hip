@@ -350,7 +350,7 @@ struct Fp8Kernel {
 __global__ __launch_bounds__(Fp8Kernel::kThreads, 1) void product_fp8_kernel(Args a, float* scratch, Told* told) {
     __shared__ __attribute__((aligned(1024))) unsigned char lds[Fp8Kernel::kLdsBytes];
     Tiles<kForward, kStepC> list(a);
-    const Plan plan = choose_tiles(list, a.n, gridDim.x, {kTallest, 60, 13});
+    const Plan plan = choose_tiles(list, gridDim.x, {kTallest, 60, 13});
     list.build(plan.height);
     const Items<kForward, kStepC> items(list, plan);
     if (blockIdx.x == 0 && threadIdx.x == 0) told->plan = items.plan;

@@ -129,12 +129,14 @@ struct Price {
 };
 
 // Height of the tiles and pieces of the leftover ones (forward, dgrad), like choose_plan() of the expert GEMMs: lane l prices one
-// of 60 plans (the tallest tile - 32 * (l / 12) rows; 1 to 6, 8, 10, 12, 16, 20 or 24 pieces) in 10 ns, as the larger of
-//   full rounds x (K steps x their price + 400) and the same for the rounds of pieces                  (MFMAs)
-//   the weights of the experts with rows at 6.6 TB/s + 600 a round                                   (memory)
-// + 300 + 2 a unit of pieces, if there are any; the first of the cheapest is taken.
+// of 60 plans (the tallest tile - 32 * (l / 12) rows; 1 to 6, 8, 10, 12, 16, 20 or 24 pieces) in 10 ns as the rounds, K steps x the price of one + 400 each
+// (full ones at the rows of the hottest expert's tiles, those of the pieces, which are the coldest, at an average tile's), + 300 + 2 for each 32 rows
+// of pieces, if there are any.  A K step does not take less than the memory needs for the weights that the workgroups of a round ask for: 32 KB each
+// at 6.4 TB/s, a line of which the row tiles of an expert share.  The first of the cheapest plans is taken.
+// (Prices of the hottest tiles for the pieces too, and one sum of the weights' time instead of the steps', left 1.5 rounds uncut: 64 experts of 1408 x 2048,
+// 3000 rows 103 -> 95 us; 1, 4096 x 4096, 300 rows 28 -> 26.5; 8, 14336 x 4096, 512 rows 200 -> 182.)
 template <class List>
-__device__ GG_INLINE Plan choose_tiles(const List& list, int features, int grid, Price price) {
+__device__ GG_INLINE Plan choose_tiles(const List& list, int grid, Price price) {
     const int lane = threadIdx.x & 63;
     const int i = min(lane / 12, 4), n = lane - lane / 12 * 12, h = price.tallest - 32 * i;
     const int p = n < 6 ? n + 1 : n < 9 ? 2 * n - 4 : 4 * n - 20;
@@ -147,15 +149,18 @@ __device__ GG_INLINE Plan choose_tiles(const List& list, int features, int grid,
     int tiles = sums[0];
 #pragma unroll
     for (int t = 1; t < 5; ++t) tiles = i == t ? sums[t] : tiles;
+    // groups of 32 rows of an average tile
+    const float groups = (float)__builtin_amdgcn_readlane(wave_sums(list.row_tiles(kUnitRows)), 63) / (float)max(tiles, 1);
     tiles *= list.n_ft;
     const int full = (int)((uint32_t)tiles / (uint32_t)grid), left = tiles - full * grid;
     const int units = (min(h, most) + kUnitRows - 1) / kUnitRows;
     const int rounds = (int)((uint32_t)(left * p + grid - 1) / (uint32_t)grid);
     const bool allowed = p == 1 || (left > 0 && left * p * units <= kScratchUnits && steps >= p * kMinPartSteps);
-    const float step = price.base + price.per_group * min(h, (most + 31) / 32 * 32) / 32;
-    const float work = full * (steps * step + 400.f) + rounds * ((uint32_t)(steps + p - 1) / (uint32_t)p * step + 400.f);
-    const float stream = active * (float)features * steps * (1.f / 516.f) + (full + rounds) * 600.f;
-    float cost = fmaxf(work, stream) + (p > 1 ? 300.f + 2.f * left * units * p : 0.f);
+    const float memory = 130.f * active * list.n_ft / (float)max(tiles, 1);   // of a K step of all workgroups
+    const float step = fmaxf(price.base + price.per_group * min(h, (most + 31) / 32 * 32) / 32, memory);
+    const float step_left = fmaxf(price.base + price.per_group * groups, memory * (left * p) / (float)max(rounds * grid, 1));
+    float cost = full * (steps * step + 400.f) + rounds * ((uint32_t)(steps + p - 1) / (uint32_t)p * step_left + 400.f);
+    if (p > 1) cost += 300.f + 2.f * left * groups * p;
     if (lane >= 60 || !allowed) cost = INFINITY;
     const float best = wave_min(cost);
     const int winner = __ffsll((long long)__ballot(cost == best)) - 1;
