@@ -12,7 +12,7 @@ hipError_t launch(const Args& a, void* workspace, hipStream_t stream) {
     const int grid = persistent_grid();
     product_gemm_kernel<FORM, OUT32><<<grid, 256, 0, stream>>>(a, scratch, told);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || !may_cut(static_cast<Form>(FORM), a, kStepC, grid)) return e;
     join_pieces_kernel<OUT32><<<kJoinWorkgroups, 256, 0, stream>>>(a.out, FORM == kForward ? a.n : a.k, a.accumulate, scratch, told);
     return hipGetLastError();
 }

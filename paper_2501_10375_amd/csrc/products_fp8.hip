@@ -365,9 +365,10 @@ __global__ __launch_bounds__(Fp8Kernel::kThreads, 1) void product_fp8_kernel(Arg
 hipError_t launch_fp8(const Args& a, void* workspace, hipStream_t stream) {
     float* scratch = static_cast<float*>(workspace);
     Told* told = reinterpret_cast<Told*>(static_cast<char*>(workspace) + kScratchBytes);
-    product_fp8_kernel<<<persistent_grid(), Fp8Kernel::kThreads, 0, stream>>>(a, scratch, told);
+    const int grid = persistent_grid();
+    product_fp8_kernel<<<grid, Fp8Kernel::kThreads, 0, stream>>>(a, scratch, told);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || !may_cut(kForward, a, kStepC, grid)) return e;
     join_pieces_kernel<false><<<kJoinWorkgroups, 256, 0, stream>>>(a.out, a.n, 0, scratch, told);
     return hipGetLastError();
 }

@@ -375,6 +375,16 @@ __device__ GG_INLINE void tell_cut(Told* told, const Item& t, int64_t out_at, in
     if (t.cut >= 0 && threadIdx.x == 0) told->cuts[t.cut] = Cut{out_at, t.rows, min(kTile, features - t.f0), t.piece, t.parts};
 }
 
+// Whether a launch of `grid` workgroups may cut tiles, as far as the host can tell: a piece has kMinPartSteps K steps at least, and wgrad cuts where its tiles
+// are fewer than the workgroups (accumulating, tiles of experts without rows do not count, which the host does not know).  Where it cannot, nothing is to be
+// joined: wgrad of 64 experts of 1408 x 2048 with 128 rows 105 -> 101 us.
+inline bool may_cut(Form form, const Args& a, int step, int grid) {
+    const int depth = form == kForward ? a.k : form == kDgrad ? a.n : a.rows;
+    if ((depth + step - 1) / step < 2 * kMinPartSteps) return false;
+    const long tiles = (long)a.experts * ((a.n + kTile - 1) / kTile) * ((a.k + kTile - 1) / kTile);
+    return form != kWgrad || a.accumulate || tiles < grid;
+}
+
 // Adds the pieces of the tiles that were cut: four rows of one of them at a time for each workgroup, a thread four columns of a row.
 constexpr int kJoinWorkgroups = 1024;
 template <bool OUT32>
