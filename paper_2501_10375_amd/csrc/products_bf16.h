@@ -61,7 +61,6 @@ struct TileKernel {
             case 16: gg::wait_vmcnt<16>(); break;
             case 20: gg::wait_vmcnt<20>(); break;
             case 24: gg::wait_vmcnt<24>(); break;
-            case 28: gg::wait_vmcnt<28>(); break;
             case 32: gg::wait_vmcnt<32>(); break;
             case 40: gg::wait_vmcnt<40>(); break;
             case 48: gg::wait_vmcnt<48>(); break;
@@ -140,26 +139,30 @@ struct TileKernel {
                 if (kQCols || n * 32 < rows) load_to(wave_lds + kQBase + stage + n * 4096, q.d, q_off[n]);
             q_next();
         };
-        // The first two K steps of an item.
-        auto request_first = [&](const Item& t) GG_LAMBDA {
-            const uint16_t *pm = static_cast<const uint16_t*>(a.p), *qm = static_cast<const uint16_t*>(a.q);
-            if constexpr (FORM == kWgrad) {
-                p.template set_columns<kStepC>(pm + (size_t)t.c0 * K + t.f0, t.depth, p_ld, (uint32_t)t.f0 * 2u, t.k_steps);
-                q.template set_columns<kStepC>(qm + (size_t)t.c0 * N + t.row0, t.depth, q_ld, (uint32_t)t.row0 * 2u, t.k_steps);
-            } else {
-                const uint16_t* matrix = pm + (size_t)t.expert * N * K;
-                if constexpr (kPCols) p.template set_columns<kStepC>(matrix + (size_t)t.c0 * K + t.f0, t.depth, p_ld, (uint32_t)t.f0 * 2u, t.k_steps);
-                else p.set_rows(matrix + (size_t)t.f0 * K + t.c0, ((int64_t)min(kTile, N - t.f0) * K - t.c0) * 2, t.k_steps);
-                const int ld = FORM == kForward ? K : N;
-                q.set_rows(qm + (size_t)t.row0 * ld + t.c0, ((int64_t)t.rows * ld - t.c0) * 2, t.k_steps);
+        // The first two K steps of an item, in four parts.
+        auto request = [&](int part, const Item& t) GG_LAMBDA {
+            if (part == 0) {
+                const uint16_t *pm = static_cast<const uint16_t*>(a.p), *qm = static_cast<const uint16_t*>(a.q);
+                if constexpr (FORM == kWgrad) {
+                    p.template set_columns<kStepC>(pm + (size_t)t.c0 * K + t.f0, t.depth, p_ld, (uint32_t)t.f0 * 2u, t.k_steps);
+                    q.template set_columns<kStepC>(qm + (size_t)t.c0 * N + t.row0, t.depth, q_ld, (uint32_t)t.row0 * 2u, t.k_steps);
+                } else {
+                    const uint16_t* matrix = pm + (size_t)t.expert * N * K;
+                    if constexpr (kPCols) p.template set_columns<kStepC>(matrix + (size_t)t.c0 * K + t.f0, t.depth, p_ld, (uint32_t)t.f0 * 2u, t.k_steps);
+                    else p.set_rows(matrix + (size_t)t.f0 * K + t.c0, ((int64_t)min(kTile, N - t.f0) * K - t.c0) * 2, t.k_steps);
+                    const int ld = FORM == kForward ? K : N;
+                    q.set_rows(qm + (size_t)t.row0 * ld + t.c0, ((int64_t)t.rows * ld - t.c0) * 2, t.k_steps);
+                }
             }
-            p_stage(0);
-            q_stage(0, t.rows);
-            p_stage(kStage);
-            q_stage(kStage, t.rows);
+            if (part % 2 == 0) p_stage(part / 2 * kStage);
+            else q_stage(part / 2 * kStage, t.rows);
+        };
+        auto request_first = [&](const Item& t) GG_LAMBDA {
+#pragma unroll
+            for (int part = 0; part < 4; ++part) request(part, t);
         };
 
-        int stores = 0;   // of the item before
+        int stores = 0;   // of the item before, behind the requests of this one
         request_first(cur);
         for (int n = 1;; ++n) {
         int tid = threadIdx.x;   // (opaque: lane addresses are computed where they are used)
@@ -261,45 +264,57 @@ struct TileKernel {
             settle();
             pin(acc);
 
-            // ---- the next item's first operands are requested before this one's results are stored.
             more_items = decode(n, next);
             gg::wait_vmcnt<0>();
             gg::lds_barrier();   // every wavefront is done reading operand tiles; no load is outstanding
-            if (more_items) request_first(next);
 
             // ---- epilogue: through LDS (8 KB a wavefront in the third stage of p, which is requested later), so that stores are whole lines.
             // An MFMA result: lane l holds row l % 16 of its fragment and features 4 * (l / 16) + 0 .. 3.  Every store is issued, whether its rows
-            // exist or not (what does not lies behind the end of the buffer), so that wait_first() can count them.
+            // exist or not (what does not lies behind the end of the buffer), so that wait_first() can count those behind the last request.
             unsigned char* own = lds + 2 * kStage + wave * 8192;
             if (!OUT32 && cur.piece < 0) {
-                // [16 rows][128 features] bf16, rows of 256 bytes, 16-byte unit u of row r at u ^ r
+                // [16 rows][128 features] bf16, rows of 256 bytes, 16-byte unit u of row r at u ^ r, in two places in turn.  The next item's first operands are
+                // requested a part ahead of each of the first four fragments' stores.  (All ahead of the first one, and one place, wgrad of 64 experts of
+                // 1408 x 2048: 64 rows each 88 us, 128 rows 101; like this 82 and 97.  In fp32, twice the bytes, it makes no difference.)
                 const int f = cur.f0 + wq * 128 + frow * 8;
                 const uint32_t stride = (uint32_t)features * 2u;
                 const __amdgpu_buffer_rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(
                     static_cast<uint16_t*>(a.out) + (FORM == kWgrad ? (size_t)cur.expert * N * K : (size_t)0) + (size_t)cur.row0 * features, 0,
                     (int)((uint32_t)cur.rows * stride), 0x00020000);
                 const uint32_t to = f < features ? (uint32_t)(wt * 16 + fpiece) * stride + (uint32_t)f * 2u : kNowhere;
-#pragma unroll
-                for (int i = 0; i < TFE; ++i) {
-                    __builtin_amdgcn_sched_barrier(0);  // one fragment's values in registers at a time
+                auto put = [&](int i) GG_LAMBDA {
 #pragma unroll
                     for (int j = 0; j < kF; ++j) {
                         uint2 pk;
                         pk.x = pack_bf16x2(from_acc(acc[j][i][0]), from_acc(acc[j][i][1]));
                         pk.y = pack_bf16x2(from_acc(acc[j][i][2]), from_acc(acc[j][i][3]));
-                        *reinterpret_cast<uint2*>(own + frow * 256 + (((j * 2 + (fpiece >> 1)) ^ frow) << 4) + (fpiece & 1) * 8) = pk;
+                        *reinterpret_cast<uint2*>(own + i % 2 * 4096 + frow * 256 + (((j * 2 + (fpiece >> 1)) ^ frow) << 4) + (fpiece & 1) * 8) = pk;
+                    }
+                };
+                constexpr int kWith = TFE < 4 ? TFE : 4;   // fragments with requests
+                put(0);
+#pragma unroll
+                for (int i = 0; i < TFE; ++i) {
+                    __builtin_amdgcn_sched_barrier(0);  // one fragment's values in registers at a time
+                    if (more_items && i < kWith) {
+#pragma unroll
+                        for (int part = i * 4 / kWith; part < (i + 1) * 4 / kWith; ++part) request(part, next);
                     }
                     gg::wave_order();
+                    u32x4 v[4];
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
                         const int lr = h * 4 + fpiece;
-                        const u32x4 v = *reinterpret_cast<const u32x4*>(own + lr * 256 + ((frow ^ lr) << 4));
-                        __builtin_amdgcn_raw_buffer_store_b128(v, out, to + (uint32_t)(i * 32 + h * 4) * stride, 0, kStreamed);
+                        v[h] = *reinterpret_cast<const u32x4*>(own + i % 2 * 4096 + lr * 256 + ((frow ^ lr) << 4));
                     }
+                    if (i + 1 < TFE) put(i + 1);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) __builtin_amdgcn_raw_buffer_store_b128(v[h], out, to + (uint32_t)(i * 32 + h * 4) * stride, 0, kStreamed);
                     gg::wave_order();
                 }
-                stores = 4 * TFE;
+                stores = 4 * (TFE - kWith + 1);
             } else {
+                if (more_items) request_first(next);
                 // [16 rows][128 features] fp32, rows of 512 bytes, 16-byte unit u of row r at u ^ r
                 const int unit = lane & 31, col = wq * 128 + unit * 4;
                 const bool piece = cur.piece >= 0;
