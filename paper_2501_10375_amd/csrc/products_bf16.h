@@ -11,6 +11,13 @@
 //            over transposed: nothing is transposed in memory, and a line of LDS is a line of memory
 // Both are loaded through buffer descriptors that begin at the K step and end at the last byte of the tile's operand, so
 // that what lies behind it (rows of a ragged tile, the end of an expert's rows in wgrad) arrives as zeros without being read.
+//
+// What bounds it: large products the MFMAs at the board's power limit (8192^3: forward and dgrad 704 us, 1.56 PFLOP/s, wgrad into fp32 755 us; a library
+// product 1.63 and, of the dgrad form, 1.40), a skewed prompt also its ragged tiles (8192 rows, 8 experts of 4096 x 14336: 725 us, 1.33 PFLOP/s, MFMAs 73 % of
+// the cycles at 1.78 GHz).  Few rows: the weights (512 rows, 8 experts of 14336 x 4096: 182 us, 5.2 TB/s).  wgrad: its result, where there are few rows (64 each,
+// 8 experts of 14336 x 4096, fp32: 335 us, 5.6 TB/s); with 1024 rows (915 us) a tile's 256 KB, which its CU's part of the L2 takes in some 10 000 cycles
+// after 16 K steps of 2 900, hold the CU up for a fifth of the time.  (Workgroups that begin at different times, so that fewer store at once, make no
+// difference: the time that they save comes back as clock.)
 #pragma once
 
 #include "products_tiles.h"
