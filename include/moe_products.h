@@ -26,6 +26,7 @@
  *     n_experts <= 64, rows <= 8388608, and one expert's matrix has less than 2^31
  *     elements.
  *   - rows == 0 is MOE_OK; the per-row buffers may then be NULL.
+ *   - An output overlaps no other buffer of its call.
  *   - Sums are held in fp32 (one rounding to the output's type).  For fp32
  *     operands the products are fp32 products, not ones of shorter formats.
  *   - NaN and infinities go where the formulas take them; rows of other experts, rows of

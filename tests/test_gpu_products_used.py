@@ -484,3 +484,70 @@ def test_layouts_are_refused():
         products.moe_grouped_product(x, o, w, y, ws[:1024])
     with pytest.raises(moe.MoeError):   # not at 16 bytes
         products.moe_grouped_product(normal(9 * 128, dtype=BF16)[4:4 + 8 * 128].view(8, 128), o, w, y, ws)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("R", [9, 700])
+@pytest.mark.parametrize("values", [[-7, 3, 5, 9], [0, 1 << 30, 2, 1 << 30], [0, 6, 0, 6], [1 << 30] * 4, [-(1 << 31), -1, 4, 4], [5, 5, 5, 5]])
+def test_tables_of_any_values_stay_inside_the_buffers(values, R, dtype):
+    """Every call on tables that leave the rows or do not ascend: nothing behind the buffers is written, and what ascends is computed."""
+    E, N, K, guard = 3, 192, 448, 64
+    offsets = torch.tensor(values, dtype=torch.int32, device=DEV)
+    x, dy, w = normal(R, K, dtype=dtype, seed=1), normal(R, N, dtype=dtype, seed=2), normal(E, N, K, dtype=dtype, seed=3)
+    ws = workspace(E, N, K, dtype, R)
+    y, dx = (torch.full((R + guard, n), UNTOUCHED, dtype=dtype, device=DEV) for n in (N, K))
+    dw = torch.full((E + 1, N, K), UNTOUCHED, device=DEV)
+    products.moe_grouped_product(x, offsets, w, y[:R], ws)
+    products.moe_grouped_product_dgrad(dy, offsets, w, dx[:R], ws)
+    products.moe_grouped_product_wgrad(dy, x, offsets, dw[:E], False, ws)
+    products.moe_grouped_product_wgrad(dy, x, offsets, dw[:E], True, ws)
+    if dtype == BF16:
+        q, s = torch.empty(R, K, dtype=torch.uint8, device=DEV), torch.empty(R, 4, device=DEV)
+        wq, wsc = torch.empty(E, N, K, dtype=torch.uint8, device=DEV), torch.empty(E, 2, 4, device=DEV)
+        y8 = torch.full((R + guard, N), UNTOUCHED, dtype=BF16, device=DEV)
+        products.moe_quantize_rows_fp8(x, q, s)
+        products.moe_quantize_weights_fp8(w, wq, wsc)
+        products.moe_grouped_product_fp8(q, s, offsets, wq, wsc, y8[:R], ws)
+        assert (y8[R:] == UNTOUCHED).all()
+    assert (y[R:] == UNTOUCHED).all() and (dx[R:] == UNTOUCHED).all() and (dw[E] == UNTOUCHED).all()
+    o = [min(max(v, 0), R) for v in values]
+    if o == sorted(o):
+        for form, got, a, depth in (("forward", y, x, K), ("dgrad", dx, dy, N)):
+            for r, want, size in reference(form, o, a, w):
+                check(got[r], want, size, depth, dtype, form)
+        for e, value, size in reference("wgrad", o, dy, x):
+            check(dw[e], 2 * value, 2 * size, 2 * (o[e + 1] - o[e]) + 1, F32, "wgrad, added to itself")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N,K", [(1 << 20, 64), (64, 1 << 20)])
+@pytest.mark.parametrize("counts", [[3, 2], [40, 300]])
+def test_the_longest_rows(counts, N, K, dtype):
+    """Features at their limit, either way, through every call."""
+    o, offsets = table(counts)
+    R, E = o[-1], 2
+    x, dy, w = normal(R, K, dtype=dtype, seed=1), normal(R, N, dtype=dtype, seed=2), normal(E, N, K, dtype=dtype, seed=3)
+    ws = workspace(E, N, K, dtype, R)
+    y, dx, dw = torch.empty(R, N, dtype=dtype, device=DEV), torch.empty(R, K, dtype=dtype, device=DEV), torch.empty(E, N, K, device=DEV)
+    products.moe_grouped_product(x, offsets, w, y, ws)
+    products.moe_grouped_product_dgrad(dy, offsets, w, dx, ws)
+    products.moe_grouped_product_wgrad(dy, x, offsets, dw, False, ws)
+    for form, got, a, depth in (("forward", y, x, K), ("dgrad", dx, dy, N)):
+        for r, want, size in reference(form, o, a, w):
+            check(got[r], want, size, depth, dtype, form)
+    for e, value, size in reference("wgrad", o, dy, x):
+        check(dw[e], value, size, counts[e], F32, "wgrad")
+    if dtype == F32:
+        return
+    kb, nb = -(-K // 128), -(-N // 128)
+    q, s = torch.empty(R, K, dtype=torch.uint8, device=DEV), torch.empty(R, kb, device=DEV)
+    wq, wsc = torch.empty(E, N, K, dtype=torch.uint8, device=DEV), torch.empty(E, nb, kb, device=DEV)
+    products.moe_quantize_rows_fp8(x, q, s)
+    products.moe_quantize_weights_fp8(w, wq, wsc)
+    products.moe_grouped_product_fp8(q, s, offsets, wq, wsc, y, ws)
+    values = q.view(torch.float8_e4m3fn).double() * s.double().repeat_interleave(128, 1)[:, :K]
+    for e in range(E):
+        r = slice(o[e], o[e + 1])
+        m = wq[e].view(torch.float8_e4m3fn).double() * wsc[e].double().repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)[:, :K]
+        want, size = values[r] @ m.T, values[r].abs() @ m.abs().T
+        assert ((y[r].double() - want).abs() <= (2.0 ** -12 + (kb + 8) * U) * size + H * want.abs()).all(), f"8 bits, expert {e}"
