@@ -7,13 +7,14 @@
 // ds_read_b32 whose four c are 16 banks apart.  The features are the instruction's first operand, so that a lane ends up with
 // four consecutive ones of a row.
 //
-// Forward and dgrad: each wavefront 16 features of all rows, so that a ragged tile costs what its groups of 16 rows cost; K steps of 32, two requested ahead
-// (the forward product of few rows: of 64, a row's 256 bytes at a time: 64 rows, 8 experts of 4096 x 4096 136 -> 121 us).  wgrad: 32 x 32 each; K steps of 16, four
-// ahead, as its contraction may be a few rows; whole rows of the result leave through LDS past the caches.
+// Forward and dgrad: each wavefront 16 features of all rows, so that a ragged tile costs what its groups of 16 rows cost; K steps of 32
+// (the forward product of few rows: of 64, a row's 256 bytes at a time).  wgrad: 32 x 32 each; K steps of 16, as its contraction may be a few rows; whole
+// rows of the result leave through LDS past the caches.  Two steps are requested ahead.
 //
-// Large products are bound by the MFMAs (1024 rows, 4096 x 4096: 113 TFLOP/s forward, 120 dgrad, 110 wgrad; a library product of 4096^3 reaches 150), those of
-// few rows by the weights (8 rows, 8 experts of 4096 x 4096: 117 us forward, 102 dgrad, 5.2 TB/s), wgrad of few rows by its result (64 rows of them: 111 us,
-// 4.8 TB/s), small ones by the time that a K step takes from its loads to its last MFMA, which
+// Large products are bound by the MFMAs (1024 rows, 4096 x 4096: 125 TFLOP/s forward, 127 dgrad, 117 wgrad, which is nine tenths of the cycles at 2.1 GHz; a
+// library product of 4096^3 reaches 150), those of few rows by the weights (64 rows, 8 experts of 4096 x 4096: 115 us forward, 106 dgrad, 5.1 TB/s), wgrad of few
+// rows by its result (64 rows of them: 107 us, 5.0 TB/s), those of about a thousand rows by the unequal shares of some six workgroups a CU (1030 rows, 16
+// experts of 1408 x 2048: 75 us each way, of which the MFMAs are half), small ones by the time that a K step takes from its loads to its last MFMA, which
 // other workgroups of a CU have to fill: where there are few, the contraction is cut and a second kernel adds the parts (8 rows of 1024 x 1024: 40 ->
 // 13 us).
 #include <type_traits>
@@ -38,39 +39,42 @@ __device__ inline void store4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) 
 
 // One operand of a tile.  ROWS: the contraction is contiguous, consecutive rows are `ld` apart; else rows are contiguous and consecutive c are
 // `ld` apart.  CUT: the contraction may end inside a K step (the rows of an expert); c from `depth` on count as zeros.
-// BK: c of a K step, AHEAD: steps that are requested ahead.
-template <bool ROWS, int TILE, bool CUT, int BK, int AHEAD>
+// BK: c of a K step.
+template <bool ROWS, int TILE, bool CUT, int BK>
 struct Operand {
     static constexpr int kAll = TILE * BK / 4, kEach = kAll < kThreads ? 1 : kAll / kThreads;   // four numbers at a time
     static constexpr int kAcross = ROWS ? BK / 4 : TILE / 4;
     static constexpr int kLd = TILE + 4, kFloats = ROWS ? TILE * BK : BK * kLd;   // of a K step in LDS
     const float* at[kEach];   // this thread's of the next K step that is requested
+    const float* base;        // CUT: some that exist
     size_t step;
-    int c_left;               // CUT: c from the first of them to the end
-    f32x4 v[AHEAD][kEach];    // K steps on their way
+    int c_left[2];            // CUT: c from the first of them to the end, of the next step in each slot
+    f32x4 v[2][kEach];        // K steps on their way, one in each slot
 
     // What a row's units are exchanged by: the 16 rows of a fragment, read at one unit, are in 64 different banks.
     static __device__ int turn(int row) { return BK == 64 ? row & 15 : BK == 32 ? row / 2 & 7 : row / 4 & 3; }
-    // `base`: element (row 0, c 0) of the tile, of which `limit` rows exist (rows behind them repeat the last one), begin: first c.
-    __device__ void set(const float* base, size_t ld, int limit, int begin, int depth) {
+    // `tile`: its element (row 0, c 0); `limit` rows of it exist (rows behind them repeat the last one); begin: first c, which is the step that goes to `first_slot`.
+    __device__ void set(const float* tile, size_t ld, int limit, int begin, int depth, int first_slot) {
 #pragma unroll
         for (int n = 0; n < kEach; ++n) {
             const int t = threadIdx.x + n * kThreads;
             const int row = ROWS ? min(t / kAcross, limit - 1) : t % kAcross * 4, c = begin + (ROWS ? t % kAcross * 4 : t / kAcross);
-            at[n] = base + (ROWS ? (size_t)row * ld + c : (size_t)c * ld + row);
+            at[n] = tile + (ROWS ? (size_t)row * ld + c : (size_t)c * ld + row);
         }
+        base = tile;
         step = ROWS ? BK : BK * ld;
-        c_left = depth - begin - threadIdx.x / kAcross;
+        const int c = depth - begin - (int)threadIdx.x / kAcross;
+        c_left[0] = first_slot == 0 ? c : c - BK;
+        c_left[1] = first_slot == 0 ? c - BK : c;
     }
     template <int SLOT>
     __device__ void load() {
 #pragma unroll
         for (int n = 0; n < kEach; ++n) {
-            v[SLOT][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if ((!CUT || c_left > n * (kThreads / kAcross)) && (kAll >= kThreads || threadIdx.x < kAll)) v[SLOT][n] = load4(at[n]);
+            v[SLOT][n] = load4(!CUT || c_left[SLOT] > n * (kThreads / kAcross) ? at[n] : base);
             at[n] += step;
         }
-        if (CUT) c_left -= BK;
+        c_left[SLOT] -= 2 * BK;
     }
     template <int SLOT>
     __device__ void stage(float* lds) const {
@@ -78,7 +82,8 @@ struct Operand {
 #pragma unroll
         for (int n = 0; n < kEach; ++n) {
             const int t = threadIdx.x + n * kThreads, a = t / kAcross, b = t % kAcross;
-            *reinterpret_cast<f32x4*>(lds + (ROWS ? a * BK + ((b ^ turn(a)) * 4) : a * kLd + b * 4)) = v[SLOT][n];
+            const bool there = !CUT || c_left[SLOT] + 2 * BK > n * (kThreads / kAcross);
+            *reinterpret_cast<f32x4*>(lds + (ROWS ? a * BK + ((b ^ turn(a)) * 4) : a * kLd + b * 4)) = there ? v[SLOT][n] : f32x4{0.f, 0.f, 0.f, 0.f};
         }
     }
     // This lane's four numbers (c half * 16 + 4 * (lane / 16) + 0 .. 3) of the fragment whose first row is `row`.
@@ -101,10 +106,9 @@ template <int FORM, int HEIGHT>
 __global__ __launch_bounds__(kThreads, 2) void product_kernel(Args a, int parts, float* scratch) {
     constexpr int kAcross = FORM == kWgrad ? 2 : 4;   // wavefronts across the features
     constexpr int kP = kTileF / 16 / kAcross, kQ = HEIGHT / 16 / (4 / kAcross);   // fragments of a wavefront
-    constexpr bool kFew = FORM == kForward && HEIGHT == 16;
-    constexpr int kBK = FORM == kWgrad ? 16 : kFew ? 64 : 32, kAhead = FORM == kWgrad ? 4 : 2;
-    using P = Operand<FORM == kForward, kTileF, FORM == kWgrad, kBK, kAhead>;
-    using Q = Operand<FORM != kWgrad, HEIGHT, FORM == kWgrad, kBK, kAhead>;
+    constexpr int kBK = FORM == kWgrad ? 16 : FORM == kForward && HEIGHT == 16 ? 64 : 32;
+    using P = Operand<FORM == kForward, kTileF, FORM == kWgrad, kBK>;
+    using Q = Operand<FORM != kWgrad, HEIGHT, FORM == kWgrad, kBK>;
     __shared__ __attribute__((aligned(16))) float lds[2][P::kFloats + Q::kFloats];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int features = FORM == kForward ? a.n : a.k;
@@ -141,9 +145,6 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(Args a, int parts,
     // This wavefront's part of the tile: row fragments wr, wr + kDown ...
     constexpr int kDown = 4 / kAcross;
     const int wf = wave % kAcross * (16 * kP), wr = wave / kAcross;
-    int fragments = FORM == kWgrad ? kQ : (rows + 15) / 16;   // of rows that exist
-    // (not a constant for the compiler: the branch keeps the MFMAs of one fragment ahead of the reads of the next, 4 % of wgrad's time)
-    if (FORM == kWgrad) asm("" : "+s"(fragments));
     f32x4 acc[kP][kQ];   // [feature fragment][row fragment]
 #pragma unroll
     for (int i = 0; i < kP; ++i)
@@ -151,49 +152,74 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(Args a, int parts,
         for (int j = 0; j < kQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int all = (depth + kBK - 1) / kBK;
     const int begin = (int)((long)all * blockIdx.y / parts), steps = (int)((long)all * (blockIdx.y + 1) / parts);
-    p.set(p_base, a.k, kTileF, begin * kBK, depth);
-    q.set(q_base, q_ld, rows, begin * kBK, depth);
-    auto request = [&](auto slot, int s) __attribute__((always_inline)) {
-        if (s >= steps) return;
-        p.template load<decltype(slot)::value>();
-        q.template load<decltype(slot)::value>();
-    };
-    auto step = [&](auto slot, int s) __attribute__((always_inline)) {
-        float *lp = lds[s & 1], *lq = lp + P::kFloats;
-        p.template stage<decltype(slot)::value>(lp);
-        q.template stage<decltype(slot)::value>(lq);
-        __syncthreads();   // (the other pair of stages is written after the next one, which everybody reaches behind its reads)
-        request(slot, s + kAhead);
+    const int first_slot = steps - begin > 1 ? (steps - begin) & 1 : 0;
+    p.set(p_base, a.k, kTileF, begin * kBK, depth, first_slot);
+    q.set(q_base, q_ld, rows, begin * kBK, depth, first_slot);
+    // All K steps, for `count` fragments of rows that exist.
+    auto compute = [&](auto count) __attribute__((always_inline)) {
+        constexpr int kCount = decltype(count)::value;
+        auto request = [&](auto slot) __attribute__((always_inline)) {
+            p.template load<decltype(slot)::value>();
+            q.template load<decltype(slot)::value>();
+        };
+        auto step = [&](auto slot, int s, auto more) __attribute__((always_inline)) {
+            float *lp = lds[s & 1], *lq = lp + P::kFloats;
+            p.template stage<decltype(slot)::value>(lp);
+            q.template stage<decltype(slot)::value>(lq);
+            __syncthreads();   // (the other pair of stages is written after the next one, which everybody reaches behind its reads)
+            if constexpr (decltype(more)::value) request(slot);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int half = 0; half < kBK / 16; ++half) {
-            f32x4 fp[kP], fq[kQ];
+            for (int half = 0; half < kBK / 16; ++half) {
+                f32x4 fp[kP], fq[kCount];
 #pragma unroll
-            for (int i = 0; i < kP; ++i) fp[i] = P::fragment(lp, wf + i * 16, half);
+                for (int i = 0; i < kP; ++i) fp[i] = P::fragment(lp, wf + i * 16, half);
 #pragma unroll
-            for (int j = 0; j < kQ; ++j) fq[j] = Q::fragment(lq, (wr + j * kDown) * 16, half);
-#pragma unroll
-            for (int j = 0; j < kQ; ++j) {
-                if (j >= fragments) break;
+                for (int j = 0; j < kCount; ++j) fq[j] = Q::fragment(lq, (wr + j * kDown) * 16, half);
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
-                    for (int i = 0; i < kP; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fp[i][c], fq[j][c], acc[i][j], 0, 0, 0);
+                    for (int j = 0; j < kCount; ++j)
+#pragma unroll
+                        for (int i = 0; i < kP; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fp[i][c], fq[j][c], acc[i][j], 0, 0, 0);
             }
+        };
+        using Zero = std::integral_constant<int, 0>;
+        using One = std::integral_constant<int, 1>;
+        using Yes = std::true_type;
+        using No = std::false_type;
+        // Two steps are requested ahead, none behind the last one, and none under a branch: a compiler that has to expect both waits for all of them.
+        int s = begin;
+        if (steps - begin == 1) {
+            request(Zero{});
+            step(Zero{}, s, No{});
+            return;
         }
+        if ((steps - begin) & 1) {
+            request(One{});
+            request(Zero{});
+            step(One{}, s++, Yes{});
+        } else {
+            request(Zero{});
+            request(One{});
+        }
+        for (; s < steps - 2; s += 2) {
+            step(Zero{}, s, Yes{});
+            step(One{}, s + 1, Yes{});
+        }
+        step(Zero{}, s, No{});
+        step(One{}, s + 1, No{});
     };
-    using std::integral_constant;
-    request(integral_constant<int, 0>{}, begin);
-    request(integral_constant<int, 1>{}, begin + 1);
-    if constexpr (kAhead == 4) {
-        request(integral_constant<int, 2>{}, begin + 2);
-        request(integral_constant<int, 3>{}, begin + 3);
-    }
-    for (int s = begin; s < steps; s += kAhead) {
-        step(integral_constant<int, 0>{}, s);
-        if (s + 1 < steps) step(integral_constant<int, 1>{}, s + 1);
-        if constexpr (kAhead == 4) {
-            if (s + 2 < steps) step(integral_constant<int, 2>{}, s + 2);
-            if (s + 3 < steps) step(integral_constant<int, 3>{}, s + 3);
+    if (begin < steps) {
+        if constexpr (FORM == kWgrad || kQ == 1) {
+            compute(std::integral_constant<int, kQ>{});
+        } else {
+            switch ((rows + 15) / 16) {
+                case 1: compute(std::integral_constant<int, 1>{}); break;
+                case 2: compute(std::integral_constant<int, 2>{}); break;
+                case 3: compute(std::integral_constant<int, 3>{}); break;
+                default: compute(std::integral_constant<int, 4>{}); break;
+            }
         }
     }
     float* out = static_cast<float*>(a.out) + out_at;
