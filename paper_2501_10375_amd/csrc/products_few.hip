@@ -135,33 +135,18 @@ namespace {
 int most_active(const Args& a) { return a.experts < a.rows ? a.experts : a.rows; }   // experts with rows
 }  // namespace
 
-// Which calls: where the experts have few rows on average, and, as long as the weights are read fast (256 MiB are what the memory-side cache
-// holds), up to 16 or 20, because a call of the tile kernels has two launches and some 10 us that are not streaming.  Times of this kernel / of
-// the tile kernels in us (experts, out, in features, rows).  bf16: 8, 14336, 4096, 16 154 / 181, 32 159 / 178, 64 181 / 190, 128 221 / 190; 8, 4096, 14336, 32
-// 192 / 187, 64 195 / 177; 64, 1408, 2048, 64 44 / 55, 300 73 / 97; 8, 4096, 4096, 64 53 / 72, 100 66 / 74; 16, 1408, 2048, 150 21 / 23; 4, 2048, 2048, 60 11 / 16, 120
-// 19 / 17; 4, 4096, 4096, 100 43 / 31; 8, 1024, 2048, 200 19 / 17; 1, 4096, 4096, 24 18 / 18.  8 bits: 8, 14336, 4096, 16 80 / 102, 64 83 / 107, 154 90 / 97 (by a skewed gate 105 / 100), 200 104 / 102;
-// 16, 6400, 4096, 32 72 / 101, 150 82 / 106, 300 91 / 88; 64, 1408, 2048, 512 41 / 47, 1024 97 / 45; 8, 2048, 2048, 150 13 / 18; 16, 1024, 1024, 300 11 / 16; 2, 6400, 4096,
-// 60 25 / 20; 1, 4096, 4096, 24 11 / 16.
-bool few_rows(const Args& a, bool fp8) {
-    const size_t bytes = (size_t)most_active(a) * a.n * a.k * (fp8 ? 1 : 2);
-    const bool cached = bytes <= (size_t)256 << 20, small = bytes <= (size_t)64 << 20;
-    return a.rows <= kRows || a.rows <= (fp8 ? 8 : 4) * a.experts ||
-           (cached && a.rows <= 320 && a.rows <= (small ? 20 : 16) * a.experts);
-}
-
-// One fragment of rows a pass up to eight rows an expert, two beyond; feature fragments that share the rows' loads where there are workgroups enough
-// (8 bits 8, 14336, 4096, 64 in ones, twos, fours: 101, 84, 83 us; 154 with two of rows: -, 106, 90; 1, 4096, 4096, 24: -, 11, 14; bf16 8, 14336, 4096, 64: 188, 203, 204).
-// Eight wavefronts where four would leave the CUs with few and each still has 16 K steps (bf16 8, 4096, 14336, 2: 42 -> 37 us; with less, 8 bits
-// 16, 6400, 4096, 2: 12.2 -> 15.4).
+// 8 bits: one fragment of rows a pass up to eight rows an expert, two beyond; feature fragments that share the rows' loads where there are workgroups enough
+// (8, 14336, 4096, 64 in ones, twos, fours: 101, 84, 83 us; 154 with two of rows: -, 106, 90; 1, 4096, 4096, 24: -, 11, 14).  bf16: one of each (8, 14336, 4096,
+// 64: 188, 203, 204), and eight wavefronts where four would leave the CUs with few and each still has 16 K steps (8, 4096, 14336, 2: 42 -> 37 us; with less,
+// 8 bits 16, 6400, 4096, 2: 12.2 -> 15.4).
 hipError_t launch_few_rows(const Args& a, bool fp8, hipStream_t stream) {
     const int active = most_active(a);
-    const bool one = a.rows <= kRows || a.rows <= 8 * a.experts;
     if (!fp8) {
         const bool eight = (long)active * (a.n / 16) <= 4L * compute_units() && a.k / 64 >= 8 * 16;
-        return !one ? launch<false, 2, 2, 4>(a, active, stream) : eight ? launch<false, 1, 1, 8>(a, active, stream) : launch<false, 1, 1, 4>(a, active, stream);
+        return eight ? launch<false, 1, 1, 8>(a, active, stream) : launch<false, 1, 1, 4>(a, active, stream);
     }
     if (a.rows <= kRows) return launch<true, 1, 1, 4>(a, active, stream);
-    if (one) return launch<true, 1, 2, 4>(a, active, stream);
+    if (a.rows <= 8 * a.experts) return launch<true, 1, 2, 4>(a, active, stream);
     return (long)active * (a.n / 64) <= 2L * compute_units() ? launch<true, 2, 2, 4>(a, active, stream) : launch<true, 2, 4, 4>(a, active, stream);
 }
 

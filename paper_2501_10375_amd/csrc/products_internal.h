@@ -81,8 +81,11 @@ constexpr size_t kScratchFloats = (size_t)8 << 20;   // parts of fp32 products
 hipError_t launch_f32(Form form, const Args& a, void* workspace, hipStream_t stream);
 hipError_t launch_bf16(Form form, const Args& a, bool out_f32, void* workspace, hipStream_t stream);
 hipError_t launch_fp8(const Args& a, void* workspace, hipStream_t stream);
-// Forward products of few rows, of bf16 or (with scales) e4m3 matrices, and which calls have few.
-bool few_rows(const Args& a, bool fp8);
+// Small products, in tiles of 64 x 64.
+constexpr int kMostSmallBlocks = 72;   // blocks of 128 of an 8-bit contraction
+hipError_t launch_small(Form form, const Args& a, bool out_f32, hipStream_t stream);
+hipError_t launch_small_fp8(const Args& a, hipStream_t stream);
+// Forward products of few rows, of bf16 or (with scales) e4m3 matrices.
 hipError_t launch_few_rows(const Args& a, bool fp8, hipStream_t stream);
 size_t product_workspace_bytes(const moe_product_t& p, int rows);
 

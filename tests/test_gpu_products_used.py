@@ -174,6 +174,16 @@ FORWARD = [   # rows of each expert, N, K: tiles of every height, several rounds
     ([150, 60], 512, 8256),                    # few tiles, a long contraction: cut
     ([500] * 9, 1024, 1024),
     ([40 + 7 * i for i in range(64)], 320, 192),
+    # sizes of the large tiles: every height, a ragged last feature tile, one round and several, cut and whole
+    ([20, 64, 70, 100, 130, 170, 200, 250], 2112, 4160),
+    ([33, 65, 97, 129, 161, 193, 225, 256, 257, 300], 4160, 2112),
+    ([1500, 900, 260, 90, 7, 0, 3, 40], 4160, 1088),
+    ([600], 2624, 8256),
+    ([5000, 0, 77], 3200, 1216),
+    # and their neighbours in tiles of 64
+    ([1, 64, 65, 0, 128, 200], 320, 4608),
+    ([63], 64, 64),
+    ([130, 2, 0, 61], 1088, 1088),
 ]
 
 
@@ -202,6 +212,11 @@ def test_rows_are_cut_in_every_way(counts, N, K, dtype):
     ([300] * 12, 1088, 1088),                  # several rounds
     ([9000], 128, 64),
     ([5 * i for i in range(64)], 192, 128),
+    # sizes of the large tiles: whole, cut, ragged, without rows
+    ([700, 0, 701, 20], 2112, 2112),
+    ([3000], 3136, 3136),
+    ([500, 3, 0, 64, 1], 3136, 1600),
+    ([63, 65, 0, 1, 128, 127, 129, 40] * 8, 512, 320),
 ])
 def test_matrices_gradients_are_cut_in_every_way(counts, N, K, dtype):
     o, offsets = table(counts, 1)
