@@ -82,7 +82,7 @@ hipError_t launch_f32(Form form, const Args& a, void* workspace, hipStream_t str
 hipError_t launch_bf16(Form form, const Args& a, bool out_f32, void* workspace, hipStream_t stream);
 hipError_t launch_fp8(const Args& a, void* workspace, hipStream_t stream);
 // Small products, in tiles of 64 x 64.
-constexpr int kMostSmallBlocks = 72;   // blocks of 128 of an 8-bit contraction
+constexpr int kMostSmallBlocks = 56;   // blocks of 128 of an 8-bit contraction (no call of more has so little to do)
 hipError_t launch_small(Form form, const Args& a, bool out_f32, hipStream_t stream);
 hipError_t launch_small_fp8(const Args& a, hipStream_t stream);
 // Forward products of few rows, of bf16 or (with scales) e4m3 matrices.

@@ -50,7 +50,7 @@ def test_loads_to_lds_do_not_follow_vector_writes_of_their_descriptors(listings)
     """A memory instruction reads a scalar register that a vector instruction wrote five wait states later at the earliest; the
     loads are asm statements, so the compiler does not see to it."""
     loads = 0
-    for name in ("product_gemm_kernel", "product_fp8_kernel"):
+    for name in ("product_gemm_kernel", "product_fp8_kernel", "product_small_kernel", "product_small_fp8_kernel"):
         for kernel, code in kernels_named(listings, name).items():
             for n, c in enumerate(code):
                 if not (c.op.startswith("buffer_load") and c.text.endswith("lds")):
