@@ -258,7 +258,7 @@ def test_fp8_rows_are_cut_in_every_way(counts, N, K):
         check(y[r], x[r] @ m.T, x[r].abs() @ m.abs().T, kb, BF16, f"expert {e}")
 
 
-@pytest.mark.parametrize("R,N,K", [(40, 320, 384), (300, 256, 640), (5, 64, 128)])
+@pytest.mark.parametrize("R,N,K", [(40, 320, 384), (300, 256, 640), (5, 64, 128), (1500, 4160, 1152), (300, 4160, 4480)])
 def test_a_row_of_bad_scales_reaches_no_other(R, N, K):
     """Blocks in odd numbers: behind a row's last scale lies the next row's first, which is NaN or infinite here in every other row."""
     x, w = normal(R, K, dtype=BF16, seed=1), normal(1, N, K, dtype=BF16, seed=3)
@@ -318,7 +318,7 @@ def same(a, b):
     return all(torch.equal(x, y) for x, y in zip(a, b, strict=True))
 
 
-MIXED = [([300, 0, 40, 9], 512, 704), ([2, 1, 0, 1], 256, 1024)]
+MIXED = [([300, 0, 40, 9], 512, 704), ([2, 1, 0, 1], 256, 1024), ([700, 0, 300, 65], 2112, 4160)]   # small tiles, few rows, large tiles
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -385,9 +385,9 @@ def test_streams_of_their_own(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-def test_buffers_begin_at_any_16_bytes(dtype):
+@pytest.mark.parametrize("counts,N,K", [([30, 0, 100, 3], 320, 448), ([300, 0, 700, 3], 2112, 4160)])
+def test_buffers_begin_at_any_16_bytes(counts, N, K, dtype):
     """Operands and results inside larger buffers, 16 bytes into them, with NaN around."""
-    counts, N, K = [30, 0, 100, 3], 320, 448
     o, offsets = table(counts)
     R, E, skip = o[-1], len(counts), 16 // torch.tensor([], dtype=dtype).element_size()
 
@@ -502,11 +502,11 @@ def test_layouts_are_refused():
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("R", [9, 700])
+@pytest.mark.parametrize("R,N,K", [(9, 192, 448), (700, 192, 448), (700, 2112, 4160)])
 @pytest.mark.parametrize("values", [[-7, 3, 5, 9], [0, 1 << 30, 2, 1 << 30], [0, 6, 0, 6], [1 << 30] * 4, [-(1 << 31), -1, 4, 4], [5, 5, 5, 5]])
-def test_tables_of_any_values_stay_inside_the_buffers(values, R, dtype):
+def test_tables_of_any_values_stay_inside_the_buffers(values, R, N, K, dtype):
     """Every call on tables that leave the rows or do not ascend: nothing behind the buffers is written, and what ascends is computed."""
-    E, N, K, guard = 3, 192, 448, 64
+    E, guard, kb, nb = 3, 64, -(-K // 128), -(-N // 128)
     offsets = torch.tensor(values, dtype=torch.int32, device=DEV)
     x, dy, w = normal(R, K, dtype=dtype, seed=1), normal(R, N, dtype=dtype, seed=2), normal(E, N, K, dtype=dtype, seed=3)
     ws = workspace(E, N, K, dtype, R)
@@ -517,8 +517,8 @@ def test_tables_of_any_values_stay_inside_the_buffers(values, R, dtype):
     products.moe_grouped_product_wgrad(dy, x, offsets, dw[:E], False, ws)
     products.moe_grouped_product_wgrad(dy, x, offsets, dw[:E], True, ws)
     if dtype == BF16:
-        q, s = torch.empty(R, K, dtype=torch.uint8, device=DEV), torch.empty(R, 4, device=DEV)
-        wq, wsc = torch.empty(E, N, K, dtype=torch.uint8, device=DEV), torch.empty(E, 2, 4, device=DEV)
+        q, s = torch.empty(R, K, dtype=torch.uint8, device=DEV), torch.empty(R, kb, device=DEV)
+        wq, wsc = torch.empty(E, N, K, dtype=torch.uint8, device=DEV), torch.empty(E, nb, kb, device=DEV)
         y8 = torch.full((R + guard, N), UNTOUCHED, dtype=BF16, device=DEV)
         products.moe_quantize_rows_fp8(x, q, s)
         products.moe_quantize_weights_fp8(w, wq, wsc)
@@ -566,3 +566,33 @@ def test_the_longest_rows(counts, N, K, dtype):
         m = wq[e].view(torch.float8_e4m3fn).double() * wsc[e].double().repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)[:, :K]
         want, size = values[r] @ m.T, values[r].abs() @ m.abs().T
         assert ((y[r].double() - want).abs() <= (2.0 ** -12 + (kb + 8) * U) * size + H * want.abs()).all(), f"8 bits, expert {e}"
+
+
+@pytest.mark.parametrize("counts,N,K", [([70, 31, 145], 320, 448), ([600, 31, 450], 2112, 4160)])
+def test_not_a_number_stays_with_its_rows_and_expert_in_every_tile(counts, N, K):
+    """NaN in a row, in an expert's matrix and behind the last row, small tiles and large: what the formulas say and nothing else."""
+    o, offsets = table(counts)
+    R = o[-1] + 3
+    x, dy, w = normal(R, K, dtype=BF16, seed=1), normal(R, N, dtype=BF16, seed=2), normal(3, N, K, dtype=BF16, seed=3)
+    x[o[-1]:], dy[o[-1]:] = math.nan, math.inf
+    x[o[1] + 5, 7], w[2, 70, 100] = math.nan, math.inf
+    ws = workspace(3, N, K, BF16, R)
+    y, dx, dw = torch.zeros(R, N, dtype=BF16, device=DEV), torch.zeros(R, K, dtype=BF16, device=DEV), torch.zeros(3, N, K, device=DEV)
+    products.moe_grouped_product(x, offsets, w, y, ws)
+    products.moe_grouped_product_dgrad(dy, offsets, w, dx, ws)
+    products.moe_grouped_product_wgrad(dy, x, offsets, dw, False, ws)
+    bad_y, bad_dx, bad_dw = (torch.zeros(t.shape, dtype=torch.bool, device=DEV) for t in (y, dx, dw))
+    bad_y[o[1] + 5], bad_y[o[2]:o[3], 70] = True, True
+    bad_dx[o[2]:o[3], 100] = True
+    bad_dw[1, :, 7] = True
+    for got, bad in ((y, bad_y), (dx, bad_dx), (dw, bad_dw)):
+        assert torch.equal(~torch.isfinite(got), bad)
+    kb, nb = -(-K // 128), -(-N // 128)
+    q, s = torch.empty(R, K, dtype=torch.uint8, device=DEV), torch.empty(R, kb, device=DEV)
+    wq, wsc = torch.empty(3, N, K, dtype=torch.uint8, device=DEV), torch.empty(3, nb, kb, device=DEV)
+    products.moe_quantize_rows_fp8(x, q, s)
+    products.moe_quantize_weights_fp8(w, wq, wsc)
+    y.zero_()
+    products.moe_grouped_product_fp8(q, s, offsets, wq, wsc, y, ws)
+    bad_y[o[2]:o[3], :128] = True    # (a tile of an expert's matrix)
+    assert torch.equal(~torch.isfinite(y), bad_y)
