@@ -58,7 +58,8 @@ enum Way { kFewRows, kSmallTiles, kLargeTiles };
 //            17; 1, 2048, 2048, 512: -, 9.5, 24; 1, 4096, 4096, 300: -, 23, 26; 8, 4096, 1024, 1000: -, 20, 21; 1, 8192, 1024, 700: -, 23, 18; 1, 2048, 2048, 2048: -, 29, 27
 //   dgrad    1, 2048, 2048, 512: -, 9.7, 24; 16, 1408, 2048, 1030: -, 21, 23; 8, 4096, 1024, 1000: -, 32, 26; 1, 1024, 8192, 700: -, 22, 20
 //   wgrad    1, 1024, 1024, 1000: -, 7.4, 25; 1, 512, 512, 4096: -, 18, 24; 1, 2048, 2048, 2048: -, 33, 47; 8, 1024, 1024, 600: -, 12, 15; of more tiles, which store more than
-//            they compute, 4, 2048, 2048, 300: -, 20, 18; 16, 1408, 2048, 30: -, 42, 24
+//            they compute, 4, 2048, 2048, 300: -, 20, 18; 16, 1408, 2048, 30: -, 42, 24; where a third of the rows, an expert's under a skewed gate, are more than 100 K
+//            steps, 64, 256, 256, 32000: -, 38, 32 (evenly 18, 27); 1, 512, 512, 8000: -, 32, 27
 //   8 bits   1, 4096, 4096, 24: 10.5, 13.1, 14; 16, 512, 4096, 100: 8.5, 13.4, 14; 1, 4096, 4096, 60: 19, 13, 17; 16, 1408, 2048, 150: 15, 11, 17; 1, 4096, 4096, 300: 88, 16, 24; 4, 2048,
 //            2048, 600: 35, 11, 16; 8, 4096, 1024, 1000: -, 17, 15; 1, 2048, 8192, 20: 16, 23, 15; 8, 14336, 4096, 64: 83, -, 107, 154 90 to 105, -, 97 to 104
 // (as long as the weights are read fast, from a memory-side cache of 256 MiB, up to 16 rows an expert are few in 8 bits).
@@ -71,7 +72,9 @@ Way choose_way(products::Form form, const Args& a, bool fp8) {
     const double down = form == kWgrad ? (double)a.experts * (a.n / 64) : a.rows / 64.0 + 0.5 * active;
     const double steps = form == kWgrad ? a.rows / (64.0 * a.experts) + 0.5 : forward ? a.k / (fp8 ? 128.0 : 64.0) : a.n / 64.0;
     const double tiles = across * down, load = (tiles < 256 ? 1.0 : tiles / 256) * (steps + 5);
-    if (fp8 ? load <= 60 && (a.k + 127) / 128 <= kMostSmallBlocks : forward ? load <= 110 : form == kDgrad ? load <= 83 : load <= 150 && tiles <= 2048) return kSmallTiles;
+    const bool deep = form == kWgrad && a.rows > 6400L * (a.experts < 3 ? a.experts : 3);
+    if (fp8 ? load <= 60 && (a.k + 127) / 128 <= kMostSmallBlocks : forward ? load <= 110 : form == kDgrad ? load <= 83 : load <= 150 && tiles <= 2048 && !deep)
+        return kSmallTiles;
     if (!forward) return kLargeTiles;
     const bool cached = (double)active * a.n * a.k <= 256.0 * (1 << 20);
     return (fp8 ? cached && a.rows <= 320 && a.rows <= 16 * a.experts : a.rows <= 4 * a.experts) ? kFewRows : kLargeTiles;
