@@ -210,15 +210,29 @@ def stage_times(fn, steps):
     return moe.moe_stage_timing_end()
 
 
-def kernel_source_digest():
-    """Short hash of the kernel sources: a stored traffic figure is only quoted for the sources it was measured on."""
-    import hashlib
+# The translation units that hold the layer's kernels and the measurement aids (not those of operators beside the layer).
+LAYER_SOURCES = ("calibrate.hip", "daop_policy.hip", "ffn_bf16.hip", "ffn_bf16_decode.hip", "ffn_f32.hip", "moe_api.hip", "permute.hip",
+                 "route.hip")
 
-    h = hashlib.sha256()
+
+def kernel_source_digest():
+    """Short hash of the layer's kernel sources and of the headers that they include from there: a stored traffic figure is
+    only quoted for the sources it was measured on."""
+    import hashlib
+    import re
+
     base = os.path.join(ROOT, "paper_2501_10375_amd", "csrc")
-    for name in sorted(os.listdir(base)):
+    texts, todo = {}, list(LAYER_SOURCES)
+    while todo:
+        name = todo.pop()
+        if name in texts or not os.path.exists(os.path.join(base, name)):
+            continue
         with open(os.path.join(base, name), "rb") as f:
-            h.update(name.encode() + b"\0" + f.read())
+            texts[name] = f.read()
+        todo += re.findall(r'^#include "([^"]+)"', texts[name].decode(), flags=re.M)
+    h = hashlib.sha256()
+    for name in sorted(texts):
+        h.update(name.encode() + b"\0" + texts[name])
     return h.hexdigest()[:16]
 
 
