@@ -92,7 +92,8 @@ int moe_grouped_product_wgrad(const moe_product_t* product, int32_t rows, const 
  * values of a row (activations), or tiles of 128 x 128 (weights); the last ones of
  * a dimension that 128 does not divide hold 64.
  *   scale  = max(largest absolute value of the block, 2^-60) / 448, rounded to nearest
- *   number = value / scale, rounded to fp32 and then to e4m3, both to nearest even
+ *   number = value / scale, rounded to fp32 and then to e4m3, both to nearest even; what becomes zero keeps
+ *            the value's sign
  * A block with an infinity or a NaN becomes NaN altogether, its scale too.
  *
  * moe_quantize_rows_fp8:    x [rows, features] -> q [rows, features], scales [rows, ceil(features / 128)]

@@ -43,7 +43,7 @@ struct Eight {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float q0 = v[i] * r;
-            q[i] = fmaf(fmaf(-q0, scale, v[i]), r, q0);
+            q[i] = fmaf(-fmaf(q0, scale, -v[i]), r, q0);   // (turned twice, so that a remainder of zero is -0, which leaves q0 its sign where that is zero too)
         }
         int lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false), hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[4], q[5], 0, false);
         lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], lo, true);
