@@ -48,46 +48,16 @@ int check_call(const moe_product_t* product, int rows, const void* const (&alway
 
 int status(hipError_t e) { return e == hipSuccess ? MOE_OK : MOE_ERR_DEVICE; }
 
-// Which kernels a bf16 or 8-bit product runs on.
-enum Way { kFewRows, kSmallTiles, kLargeTiles };
-
-// The host knows the rows of a call, not of its experts: their tiles of 64 rows are taken to be rows / 64 and half a tile for each expert.  A workgroup of the small
-// tiles takes its K steps and what five of them would take, and every CU as many workgroups as there are for each of them; the large tiles are planned and
-// joined first, and read less for an MFMA.  Of few rows the experts' weights are a stream.  Times in us (experts, out, in features, rows), few rows / small / large:
-//   forward  4, 2048, 2048, 16: 7.8, 8.9, 14; 1, 4096, 4096, 24: 17, 14.8, 15; 8, 4096, 4096, 64: 48, 41, 48; 64, 1408, 2048, 64: 34, 33, 35; 1, 1024, 1024, 1000: -, 7.1,
-//            17; 1, 2048, 2048, 512: -, 9.5, 24; 1, 4096, 4096, 300: -, 23, 26; 8, 4096, 1024, 1000: -, 20, 21; 1, 8192, 1024, 700: -, 23, 18; 1, 2048, 2048, 2048: -, 29, 27
-//   dgrad    1, 2048, 2048, 512: -, 9.7, 24; 16, 1408, 2048, 1030: -, 21, 23; 8, 4096, 1024, 1000: -, 32, 26; 1, 1024, 8192, 700: -, 22, 20
-//   wgrad    1, 1024, 1024, 1000: -, 7.4, 25; 1, 512, 512, 4096: -, 18, 24; 1, 2048, 2048, 2048: -, 33, 47; 8, 1024, 1024, 600: -, 12, 15; of more tiles, which store more than
-//            they compute, 4, 2048, 2048, 300: -, 20, 18; 16, 1408, 2048, 30: -, 42, 24; where a third of the rows, an expert's under a skewed gate, are more than 100 K
-//            steps, 64, 256, 256, 32000: -, 38, 32 (evenly 18, 27); 1, 512, 512, 8000: -, 32, 27
-//   8 bits   1, 4096, 4096, 24: 10.5, 13.1, 14; 16, 512, 4096, 100: 8.5, 13.4, 14; 1, 4096, 4096, 60: 19, 13, 17; 16, 1408, 2048, 150: 15, 11, 17; 1, 4096, 4096, 300: 88, 16, 24; 4, 2048,
-//            2048, 600: 35, 11, 16; 8, 4096, 1024, 1000: -, 17, 15; 1, 2048, 8192, 20: 16, 23, 15; 8, 14336, 4096, 64: 83, -, 107, 154 90 to 105, -, 97 to 104
-// (as long as the weights are read fast, from a memory-side cache of 256 MiB, up to 16 rows an expert are few in 8 bits).
-Way choose_way(products::Form form, const Args& a, bool fp8) {
-    using namespace products;
-    const bool forward = form == kForward;
-    if (forward && (a.rows <= (fp8 ? 32 : 16) || (fp8 && a.rows <= 8 * a.experts))) return kFewRows;
-    const double active = a.experts < a.rows ? a.experts : a.rows;
-    const double across = forward ? a.n / 64 : a.k / 64;
-    const double down = form == kWgrad ? (double)a.experts * (a.n / 64) : a.rows / 64.0 + 0.5 * active;
-    const double steps = form == kWgrad ? a.rows / (64.0 * a.experts) + 0.5 : forward ? a.k / (fp8 ? 128.0 : 64.0) : a.n / 64.0;
-    const double tiles = across * down, load = (tiles < 256 ? 1.0 : tiles / 256) * (steps + 5);
-    const bool deep = form == kWgrad && a.rows > 6400L * (a.experts < 3 ? a.experts : 3);
-    if (fp8 ? load <= 60 && (a.k + 127) / 128 <= kMostSmallBlocks : forward ? load <= 110 : form == kDgrad ? load <= 83 : load <= 150 && tiles <= 2048 && !deep)
-        return kSmallTiles;
-    if (!forward) return kLargeTiles;
-    const bool cached = (double)active * a.n * a.k <= 256.0 * (1 << 20);
-    return (fp8 ? cached && a.rows <= 320 && a.rows <= 16 * a.experts : a.rows <= 4 * a.experts) ? kFewRows : kLargeTiles;
-}
+products::Size size_of(const Args& a) { return {a.experts, a.rows, a.n, a.k}; }
 
 int enqueue(products::Form form, const moe_product_t& p, int32_t rows, const void* q, const void* second, const int32_t* offsets,
             void* out, bool out_f32, int accumulate, void* workspace, void* hip_stream) {
     const Args a = {q, second, out, offsets, p.n_experts, rows, p.out_features, p.in_features, nullptr, nullptr, accumulate};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (p.dtype == MOE_F32) return status(products::launch_f32(form, a, workspace, stream));
-    switch (choose_way(form, a, false)) {
-        case kFewRows: return status(products::launch_few_rows(a, false, stream));
-        case kSmallTiles: return status(products::launch_small(form, a, out_f32, stream));
+    switch (products::choose_way(form, size_of(a), false)) {
+        case products::kFewRows: return status(products::launch_few_rows(a, false, stream));
+        case products::kSmallTiles: return status(products::launch_small(form, a, out_f32, stream));
         default: return status(products::launch_bf16(form, a, out_f32, workspace, stream));
     }
 }
@@ -163,9 +133,9 @@ int moe_grouped_product_fp8(const moe_product_t* product, int32_t rows, const ui
     if (rows == 0) return MOE_OK;
     const Args a = {xq, wq, y, offsets, product->n_experts, rows, product->out_features, product->in_features, x_scales, w_scales, 0};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    switch (choose_way(products::kForward, a, true)) {
-        case kFewRows: return status(products::launch_few_rows(a, true, stream));
-        case kSmallTiles: return status(products::launch_small_fp8(a, stream));
+    switch (products::choose_way(products::kForward, size_of(a), true)) {
+        case products::kFewRows: return status(products::launch_few_rows(a, true, stream));
+        case products::kSmallTiles: return status(products::launch_small_fp8(a, stream));
         default: return status(products::launch_fp8(a, workspace, stream));
     }
 }

@@ -131,23 +131,12 @@ hipError_t launch(const Args& a, int active, hipStream_t stream) {
 
 }  // namespace
 
-namespace {
-int most_active(const Args& a) { return a.experts < a.rows ? a.experts : a.rows; }   // experts with rows
-}  // namespace
-
-// 8 bits: one fragment of rows a pass up to eight rows an expert, two beyond; feature fragments that share the rows' loads where there are workgroups enough
-// (8, 14336, 4096, 64 in ones, twos, fours: 101, 84, 83 us; 154 with two of rows: -, 106, 90; 1, 4096, 4096, 24: -, 11, 14).  bf16: one of each (8, 14336, 4096,
-// 64: 188, 203, 204), and eight wavefronts where four would leave the CUs with few and each still has 16 K steps (8, 4096, 14336, 2: 42 -> 37 us; with less,
-// 8 bits 16, 6400, 4096, 2: 12.2 -> 15.4).
 hipError_t launch_few_rows(const Args& a, bool fp8, hipStream_t stream) {
-    const int active = most_active(a);
-    if (!fp8) {
-        const bool eight = (long)active * (a.n / 16) <= 4L * compute_units() && a.k / 64 >= 8 * 16;
-        return eight ? launch<false, 1, 1, 8>(a, active, stream) : launch<false, 1, 1, 4>(a, active, stream);
-    }
-    if (a.rows <= kRows) return launch<true, 1, 1, 4>(a, active, stream);
-    if (a.rows <= 8 * a.experts) return launch<true, 1, 2, 4>(a, active, stream);
-    return (long)active * (a.n / 64) <= 2L * compute_units() ? launch<true, 2, 2, 4>(a, active, stream) : launch<true, 2, 4, 4>(a, active, stream);
+    const int active = a.experts < a.rows ? a.experts : a.rows;
+    const FewRows v = choose_few_rows({a.experts, a.rows, a.n, a.k}, fp8, compute_units());
+    if (!fp8) return v.waves == 8 ? launch<false, 1, 1, 8>(a, active, stream) : launch<false, 1, 1, 4>(a, active, stream);
+    if (v.row_fragments == 1) return v.feature_fragments == 1 ? launch<true, 1, 1, 4>(a, active, stream) : launch<true, 1, 2, 4>(a, active, stream);
+    return v.feature_fragments == 2 ? launch<true, 2, 2, 4>(a, active, stream) : launch<true, 2, 4, 4>(a, active, stream);
 }
 
 }  // namespace products

@@ -7,15 +7,10 @@
 
 #include "moe_internal.h"
 #include "moe_products.h"
+#include "products_rules.h"
 
 namespace moe {
 namespace products {
-
-// What a product computes, as out[row, feature] = sum over c of q(row, c) * p(feature, c):
-//   kForward  q = x,  p = W_e,    c = in_features
-//   kDgrad    q = dy, p = W_e^T,  c = out_features
-//   kWgrad    q = dy^T, p = x^T,  c = the rows of expert e; an output matrix for every expert
-enum Form { kForward, kDgrad, kWgrad };
 
 struct Args {
     const void *q, *p;
@@ -82,7 +77,6 @@ hipError_t launch_f32(Form form, const Args& a, void* workspace, hipStream_t str
 hipError_t launch_bf16(Form form, const Args& a, bool out_f32, void* workspace, hipStream_t stream);
 hipError_t launch_fp8(const Args& a, void* workspace, hipStream_t stream);
 // Small products, in tiles of 64 x 64.
-constexpr int kMostSmallBlocks = 56;   // blocks of 128 of an 8-bit contraction (no call of more has so little to do)
 hipError_t launch_small(Form form, const Args& a, bool out_f32, hipStream_t stream);
 hipError_t launch_small_fp8(const Args& a, hipStream_t stream);
 // Forward products of few rows, of bf16 or (with scales) e4m3 matrices.
