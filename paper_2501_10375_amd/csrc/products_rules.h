@@ -17,7 +17,7 @@ struct Size {
 // Which kernels a bf16 or 8-bit product runs on.
 enum Way { kFewRows, kSmallTiles, kLargeTiles };
 
-// Blocks of 128 of an 8-bit contraction that the small tiles' kernel has room for (no call of more has so little to do).
+// Blocks of 128 of an 8-bit contraction that the small tiles' kernel has room for.  (A guard: the rule below, which allows 60 K steps less five, asks for 55 at most.)
 constexpr int kMostSmallBlocks = 56;
 
 // The host knows the rows of a call, not of its experts: their tiles of 64 rows are taken to be rows / 64 and half a tile for each expert.  A workgroup of the small

@@ -14,3 +14,5 @@ extern "C" int products_few_rows(int fp8, int experts, int rows, int n, int k, i
     out[2] = v.waves;
     return 0;
 }
+
+extern "C" int products_most_small_blocks() { return kMostSmallBlocks; }

@@ -24,3 +24,6 @@ FEW_ROWS_FP8 = [
     (([40] + [8] * 7, 8192, 2240), (2, 4, 4)),                # two passes, the last block of 64
     (([33, 0, 66, 0, 0, 0, 0, 1], 8192, 2304), (2, 4, 4)),    # three, of one expert two
 ]
+# The small tiles' longest contractions in 8 bits (its scales have room for 56 blocks), and what lies behind them.
+SMALL_FP8 = [([40], 64, 7040), ([70], 320, 7040), ([40], 64, 6976), ([100, 0, 33], 320, 6976)]
+BEHIND_SMALL_FP8 = [([40], 64, 7104), ([70], 320, 7168)]

@@ -1,4 +1,5 @@
-"""Grouped products at shapes that are known to reach each variant of the few-row kernel, with more rows of an expert than a pass serves (see test_products_rules.py for which shape takes
+"""Grouped products at shapes that are known to reach each variant of the few-row kernel, with more rows of an expert than a pass serves and the longest
+contractions of the small 8-bit tiles (see test_products_rules.py for which shape takes
 which).  Tolerances as in test_gpu_products.py."""
 import math
 
@@ -6,13 +7,13 @@ import pytest
 import torch
 
 from paper_2501_10375_amd import products
-from products_shapes import FEW_ROWS_BF16, FEW_ROWS_FP8
+from products_shapes import BEHIND_SMALL_FP8, FEW_ROWS_BF16, FEW_ROWS_FP8, SMALL_FP8
 from test_gpu_products import BF16, DEV, UNTOUCHED, check, normal, reference, table, workspace
 
 pytestmark = pytest.mark.gpu
 U, H = 2.0 ** -24, 2.0 ** -8
 E4M3 = torch.float8_e4m3fn
-FP8 = [shape for shape, _ in FEW_ROWS_FP8]
+FP8 = [shape for shape, _ in FEW_ROWS_FP8] + SMALL_FP8 + BEHIND_SMALL_FP8
 
 
 def label(v):

@@ -9,7 +9,7 @@ import pytest
 
 import test_gpu_products as basic
 import test_gpu_products_used as used
-from products_shapes import FEW_ROWS_BF16, FEW_ROWS_FP8
+from products_shapes import BEHIND_SMALL_FP8, FEW_ROWS_BF16, FEW_ROWS_FP8, SMALL_FP8
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(os.path.dirname(HERE), "paper_2501_10375_amd", "csrc")
@@ -63,6 +63,23 @@ def test_every_variant_of_few_rows_has_shapes_of_several_passes(rules):
         for (counts, _, _), v in cases:
             tested[v] = tested.get(v, False) or max(counts) > 16 * v[0]
         assert tested == seen[fp8], "bf16 8 bits".split()[fp8]
+
+
+def test_shapes_at_the_end_of_the_small_tiles(rules):
+    for counts, N, K in SMALL_FP8:
+        assert way(rules, FORWARD, True, len(counts), sum(counts), N, K) == SMALL
+    for counts, N, K in BEHIND_SMALL_FP8:
+        assert way(rules, FORWARD, True, len(counts), sum(counts), N, K) == LARGE
+    assert max(-(-K // 128) for _, _, K in SMALL_FP8) == 55
+
+
+def test_no_call_brings_the_small_tiles_more_blocks_than_they_have_room_for(rules):
+    room = rules.products_most_small_blocks()
+    for K in range(64, 16384, 64):
+        for R in (9, 33, 100):
+            for E, N in ((1, 64), (3, 64), (1, 4096)):
+                if way(rules, FORWARD, True, E, R, N, K) == SMALL:
+                    assert -(-K // 128) < room
 
 
 def test_every_form_has_tested_shapes_of_every_way(rules):
