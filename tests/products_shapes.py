@@ -27,3 +27,5 @@ FEW_ROWS_FP8 = [
 # The small tiles' longest contractions in 8 bits (its scales have room for 56 blocks), and what lies behind them.
 SMALL_FP8 = [([40], 64, 7040), ([70], 320, 7040), ([40], 64, 6976), ([100, 0, 33], 320, 6976)]
 BEHIND_SMALL_FP8 = [([40], 64, 7104), ([70], 320, 7168)]
+# Products whose rows' gradient in 8 bits (the product of exchanged features) takes each way.
+GRADIENT_FP8 = [([2, 0, 5], 320, 448, "few"), ([70, 0, 31], 448, 192, "small"), ([600, 31, 450], 2112, 4160, "large"), ([1000, 0, 1], 4160, 2112, "large")]

@@ -1,5 +1,5 @@
-"""Grouped products at shapes that are known to reach each variant of the few-row kernel, with more rows of an expert than a pass serves and the longest
-contractions of the small 8-bit tiles (see test_products_rules.py for which shape takes
+"""Grouped products at shapes that are known to reach each variant of the few-row kernel, with more rows of an expert than a pass serves, the longest
+contractions of the small 8-bit tiles, and gradients of rows in 8 bits through every kernel (see test_products_rules.py for which shape takes
 which).  Tolerances as in test_gpu_products.py."""
 import math
 
@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2501_10375_amd import products
-from products_shapes import BEHIND_SMALL_FP8, FEW_ROWS_BF16, FEW_ROWS_FP8, SMALL_FP8
+from products_shapes import BEHIND_SMALL_FP8, FEW_ROWS_BF16, FEW_ROWS_FP8, GRADIENT_FP8, SMALL_FP8
 from test_gpu_products import BF16, DEV, UNTOUCHED, check, normal, reference, table, workspace
 
 pytestmark = pytest.mark.gpu
@@ -94,3 +94,26 @@ def test_not_a_number_in_8_bits_stays_in_its_row_from_pass_to_pass(counts, N, K)
     xs[bad, kb - 1] = math.inf      # and an infinite scale
     products.moe_grouped_product_fp8(xq, xs, offsets, wq, wsc, y, ws)
     assert not torch.isfinite(y[bad]).any() and torch.equal(y[~bad], want[~bad])
+
+
+@pytest.mark.parametrize("counts,N,K,kernel", GRADIENT_FP8, ids=label)
+def test_gradients_of_rows_in_8_bits(counts, N, K, kernel):
+    """dx of a product in 8 bits: the product of quantised dy with the transposed weights and exchanged features."""
+    E, (o, offsets) = len(counts), table(counts)
+    R, nb, kb = o[-1], -(-N // 128), -(-K // 128)
+    w, dy = normal(E, N, K, dtype=BF16, seed=3), normal(R, N, dtype=BF16, seed=2)
+    q, q_t = (torch.empty(s, dtype=torch.uint8, device=DEV) for s in ((E, N, K), (E, K, N)))
+    s, s_t = torch.empty(E, nb, kb, device=DEV), torch.empty(E, kb, nb, device=DEV)
+    products.moe_quantize_weights_fp8(w, q, s, q_t, s_t)
+    dq, ds = torch.empty(R, N, dtype=torch.uint8, device=DEV), torch.empty(R, nb, device=DEV)
+    products.moe_quantize_rows_fp8(dy, dq, ds)
+    dx = torch.full((R + 1, K), UNTOUCHED, dtype=BF16, device=DEV)
+    products.moe_grouped_product_fp8(dq, ds, offsets, q_t, s_t, dx[:R], workspace(E, K, N, BF16, R))
+    assert (dx[R] == UNTOUCHED).all()
+    values = dq.view(E4M3).double() * spread(ds, 1, R, N)
+    for e in range(E):
+        r = slice(o[e], o[e + 1])
+        m = q[e].view(E4M3).double() * spread(s[e], 128, N, K)
+        want, size = values[r] @ m, values[r].abs() @ m.abs()
+        tol = (7 * 2.0 ** -13 + 2.0 ** -18 + (nb + 8) * U) * size + H * want.abs()
+        assert ((dx[r].double() - want).abs() <= tol).all(), f"expert {e}"

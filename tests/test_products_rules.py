@@ -9,7 +9,7 @@ import pytest
 
 import test_gpu_products as basic
 import test_gpu_products_used as used
-from products_shapes import BEHIND_SMALL_FP8, FEW_ROWS_BF16, FEW_ROWS_FP8, SMALL_FP8
+from products_shapes import BEHIND_SMALL_FP8, FEW_ROWS_BF16, FEW_ROWS_FP8, GRADIENT_FP8, SMALL_FP8
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(os.path.dirname(HERE), "paper_2501_10375_amd", "csrc")
@@ -80,6 +80,11 @@ def test_no_call_brings_the_small_tiles_more_blocks_than_they_have_room_for(rule
             for E, N in ((1, 64), (3, 64), (1, 4096)):
                 if way(rules, FORWARD, True, E, R, N, K) == SMALL:
                     assert -(-K // 128) < room
+
+
+def test_gradient_shapes_take_their_way(rules):
+    for counts, N, K, name in GRADIENT_FP8:
+        assert way(rules, FORWARD, True, len(counts), sum(counts), K, N) == {"few": FEW, "small": SMALL, "large": LARGE}[name]
 
 
 def test_every_form_has_tested_shapes_of_every_way(rules):
