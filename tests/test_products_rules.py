@@ -104,3 +104,16 @@ def test_every_form_has_tested_shapes_of_every_way(rules):
     # one call after another, replays and streams: small tiles, few rows, large tiles
     mixed = [[way(rules, FORWARD, fp8, len(c), sum(c), N, K) for c, N, K in used.MIXED] for fp8 in (False, True)]
     assert mixed == [[SMALL, FEW, LARGE]] * 2
+
+
+def test_one_workspace_serves_every_shape_of_a_type():
+    import torch
+
+    from paper_2501_10375_amd import build, moe, products
+
+    if not os.path.exists(moe.LIB_PATH):
+        build.build()
+    for dtype, size in ((torch.bfloat16, 66.9e6), (torch.float32, 33.6e6)):
+        sizes = {products.moe_product_workspace_bytes(products.make_product(E, N, K, dtype), rows)
+                 for E, N, K in ((1, 64, 64), (8, 14336, 4096), (8, 4096, 14336), (64, 1408, 2048), (1, 64, 1 << 20)) for rows in (0, 1, 300, 8192, 1 << 23)}
+        assert len(sizes) == 1 and abs(sizes.pop() - size) < 0.1e6
