@@ -12,7 +12,7 @@
 // rows of the result leave through LDS past the caches.  Two steps are requested ahead.
 //
 // Large products are bound by the MFMAs (1024 rows, 4096 x 4096: 125 TFLOP/s forward, 127 dgrad, 117 wgrad, which is nine tenths of the cycles at 2.1 GHz; a
-// library product of 4096^3 reaches 150), those of few rows by the weights (64 rows, 8 experts of 4096 x 4096: 115 us forward, 106 dgrad, 5.1 TB/s), wgrad of few
+// library product of 4096^3 reaches 150), those of few rows by the weights (64 rows, 8 experts of 4096 x 4096: 115 us forward, 4.7 TB/s, 106 dgrad, 5.1), wgrad of few
 // rows by its result (64 rows of them: 107 us, 5.0 TB/s), those of about a thousand rows by the unequal shares of some six workgroups a CU (1030 rows, 16
 // experts of 1408 x 2048: 75 us each way, of which the MFMAs are half), small ones by the time that a K step takes from its loads to its last MFMA, which
 // other workgroups of a CU have to fill: where there are few, the contraction is cut and a second kernel adds the parts (8 rows of 1024 x 1024: 40 ->

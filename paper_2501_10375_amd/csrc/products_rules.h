@@ -20,18 +20,38 @@ enum Way { kFewRows, kSmallTiles, kLargeTiles };
 // Blocks of 128 of an 8-bit contraction that the small tiles' kernel has room for.  (A guard: the rule below, which allows 60 K steps less five, asks for 55 at most.)
 constexpr int kMostSmallBlocks = 56;
 
-// The host knows the rows of a call, not of its experts: their tiles of 64 rows are taken to be rows / 64 and half a tile for each expert.  A workgroup of the small
-// tiles takes its K steps and what five of them would take, and every CU as many workgroups as there are for each of them; the large tiles are planned and
-// joined first, and read less for an MFMA.  Of few rows the experts' weights are a stream.  Times in us (experts, out, in features, rows), few rows / small / large:
-//   forward  4, 2048, 2048, 16: 7.8, 8.9, 14; 1, 4096, 4096, 24: 17, 14.8, 15; 8, 4096, 4096, 64: 48, 41, 48; 64, 1408, 2048, 64: 34, 33, 35; 1, 1024, 1024, 1000: -, 7.1,
-//            17; 1, 2048, 2048, 512: -, 9.5, 24; 1, 4096, 4096, 300: -, 23, 26; 8, 4096, 1024, 1000: -, 20, 21; 1, 8192, 1024, 700: -, 23, 18; 1, 2048, 2048, 2048: -, 29, 27
-//   dgrad    1, 2048, 2048, 512: -, 9.7, 24; 16, 1408, 2048, 1030: -, 21, 23; 8, 4096, 1024, 1000: -, 32, 26; 1, 1024, 8192, 700: -, 22, 20
-//   wgrad    1, 1024, 1024, 1000: -, 7.4, 25; 1, 512, 512, 4096: -, 18, 24; 1, 2048, 2048, 2048: -, 33, 47; 8, 1024, 1024, 600: -, 12, 15; of more tiles, which store more than
-//            they compute, 4, 2048, 2048, 300: -, 20, 18; 16, 1408, 2048, 30: -, 42, 24; where a third of the rows, an expert's under a skewed gate, are more than 100 K
-//            steps, 64, 256, 256, 32000: -, 38, 32 (evenly 18, 27); 1, 512, 512, 8000: -, 32, 27
-//   8 bits   1, 4096, 4096, 24: 10.5, 13.1, 14; 16, 512, 4096, 100: 8.5, 13.4, 14; 1, 4096, 4096, 60: 19, 13, 17; 16, 1408, 2048, 150: 15, 11, 17; 1, 4096, 4096, 300: 88, 16, 24; 4, 2048,
-//            2048, 600: 35, 11, 16; 8, 4096, 1024, 1000: -, 17, 15; 1, 2048, 8192, 20: 16, 23, 15; 8, 14336, 4096, 64: 83, -, 107, 154 90 to 105, -, 97 to 104
-// (as long as the weights are read fast, from a memory-side cache of 256 MiB, up to 16 rows an expert are few in 8 bits).
+// The host knows the rows of a call, not of its experts: their tiles of 64 rows are taken to be rows / 64 and half a tile for each expert.  A workgroup of
+// the small tiles takes its K steps and what five of them would take, and every CU as many workgroups as there are for each of them; the large tiles are
+// planned and joined first, and read less for an MFMA.  Of few rows the experts' weights are a stream; as long as they are read fast, from a memory-side cache of
+// 256 MiB, up to 16 rows an expert are few in 8 bits.  Times in us, * what the rule takes, routed evenly or
+// mildly skewed (Zipf 0.5 to 0.8) unless noted:
+//
+//   experts, out, in, rows            few rows  small  large        experts, out, in, rows            small  large
+//   forward  4, 2048, 2048, 16           7.8*     8.9    14         dgrad  1, 2048, 2048, 512           9.7*    24
+//            1, 4096, 4096, 24          17       14.8*   15                16, 1408, 2048, 1030        21*      23
+//            8, 4096, 4096, 64          48       41*     48                8, 4096, 1024, 1000         32       26*
+//            64, 1408, 2048, 128        62       71*     84                1, 1024, 8192, 700          22       20*
+//            64, 1408, 2048, 256        64*      71      85         wgrad  1, 1024, 1024, 1000          7.4*    25
+//            1, 1024, 1024, 1000         -        7.1*   17                1, 512, 512, 4096           18*      24
+//            1, 4096, 4096, 300          -       23*     26                1, 2048, 2048, 2048         33*      47
+//            1, 8192, 1024, 700          -       23      18*               8, 1024, 1024, 600          12*      15
+//            1, 2048, 2048, 2048         -       29      27*               4, 2048, 2048, 300 (*)      20       18*
+//   8 bits   1, 4096, 4096, 24          10.5*    13.1    14                16, 1408, 2048, 30 (*)      42       24*
+//            1, 2048, 8192, 20          16*      23      15                64, 256, 256, 19200         13.8*    17
+//            1, 4096, 4096, 60          19       13*     17                  the same, Zipf 1.2        26*      30
+//            16, 1408, 2048, 128        10.8*    11.2    16                64, 256, 256, 32000         18.7     27*
+//            16, 1408, 2048, 150 (Z)    15       11*     17                  the same, Zipf 1.2        38       32*
+//            64, 1408, 2048, 512        32*      33      35                1, 512, 512, 8000           32       28*
+//            16, 512, 4096, 128          8.5*    13.4    14         (*) many tiles, which store more than they compute; (Z) Zipf 1.2
+//            4, 2048, 2048, 600         35       11*     16
+//            8, 4096, 1024, 1000         -       17      15*
+//            8, 14336, 4096, 64         83*       -     107
+//            8, 14336, 4096, 154        90 to 105 -      97 to 104*
+//
+// What the host does not see is the skew, and the rule pays for it where it is strong.  Few rows read an expert's weights again for every 16 of its rows: 64 experts of
+// 1408 x 2048 with Zipf 1.2, 8 bits, 512 rows 67 where small tiles take 31, bf16, 256 rows 72 (43); all rows on one expert 102 (8.5) and 63 (9.0).  wgrad of more than
+// 6400 rows for each of up to three experts is taken to have an expert with a third of them, more K steps than a workgroup of the small tiles should have: evenly routed
+// it is half as slow again.
 inline Way choose_way(Form form, const Size& a, bool fp8) {
     const bool forward = form == kForward;
     if (forward && (a.rows <= (fp8 ? 32 : 16) || (fp8 && a.rows <= 8 * a.experts))) return kFewRows;
